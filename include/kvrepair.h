@@ -250,6 +250,107 @@ kvr_status kvr_margin(kvr_model *model, const kvr_cache *cache, const int32_t *p
 kvr_status kvr_logits(kvr_model *model, const kvr_cache *cache, const int32_t *query, int32_t m,
                       float *logits_out);
 
+/* ---- documents held in 4 bits ----
+ *
+ * A packed cache holds a document's K/V in 4.5 bits an entry, 0.28 of a bf16
+ * cache.  Groups of 16 consecutive entries of head_dim share a scale: a sixth of
+ * the group's largest magnitude, rounded (to nearest, ties to even) to 5
+ * exponent and 3 mantissa bits, 2^-17 to 10240 (larger groups saturate).  An
+ * entry is one of {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign times the scale: the one
+ * nearest to it (ties to the even code), exact in bf16 and fp32.  A row (position,
+ * KV head, K or V) holding a NaN or an infinity reads back as NaN throughout.
+ *
+ * Beside each block of KVR_BLOCK positions of a KV head the cache keeps bounds of its
+ * keys: for each entry of head_dim the largest and the least value over the
+ * block's finite rows, as whole numbers hi (rounded up) and lo (down) of
+ * `unit`, the smallest power of two (at least 2^-100) with every magnitude <=
+ * 127 unit.
+ *
+ * k, v, q, out and block arrays are DEVICE pointers (16-byte aligned, of the model's
+ * device, in the model dtype resp. int32) that the caller owns; positions are
+ * host arrays, read during the call.  Calls are asynchronous on the model's stream
+ * and allocate nothing once the model's scratch fits, unless stated.  Handles are
+ * the library's; kvr_model_free frees those still live. */
+#define KVR_BLOCK 64
+
+typedef struct kvr_packed kvr_packed;
+typedef struct kvr_rows kvr_rows;
+
+/* An empty packed cache for up to `capacity` positions (1 .. 2^20; past the
+ * model's max_context only these calls reach them) of every layer.  Errors:
+ * KVR_E_INVAL, KVR_E_RANGE, KVR_E_NOMEM. */
+kvr_status kvr_packed_create(kvr_model *model, int32_t capacity, kvr_packed **out);
+/* Waits for the model's stream.  Rows over the document (below) become invalid. */
+void kvr_packed_free(kvr_packed *packed);
+/* Positions written so far (the highest plus one); -1 for NULL. */
+int32_t kvr_packed_len(const kvr_packed *packed);
+
+/* Quantise the rows of `positions` (strictly increasing, in [0, capacity), none past
+ * the first position not yet written plus those before it in the call) for layers
+ * [layer_begin, layer_end) into the cache: k, v [n_pos][layers][n_kv_heads][head_dim].
+ * Rewritten positions are replaced, and the bounds of the touched blocks are taken
+ * anew over all their rows.  A layer whose rows of a position were not
+ * written holds zeros there.  n_pos == 0 or no layers: nothing is done.  Errors: KVR_E_INVAL (NULL
+ * or not device memory, alignment), KVR_E_RANGE (layers, positions),
+ * KVR_E_POISONED, KVR_E_NOMEM, KVR_E_CUDA (poisons the cache). */
+kvr_status kvr_packed_write(kvr_packed *packed, const int32_t *positions, int32_t n_pos,
+                            int32_t layer_begin, int32_t layer_end, const void *k, const void *v);
+
+/* The rows of `positions` (strictly increasing, in [0, length)) as stored, widened to
+ * the model dtype (exactly): k_out, v_out [n_pos][layers][n_kv_heads][head_dim].
+ * Errors as kvr_packed_write. */
+kvr_status kvr_packed_read(const kvr_packed *packed, const int32_t *positions, int32_t n_pos,
+                           int32_t layer_begin, int32_t layer_end, void *k_out, void *v_out);
+
+/* The bounds of one layer, to host memory: hi, lo [n_kv_heads][blocks][head_dim], unit
+ * [n_kv_heads][blocks], blocks = ceil(length / KVR_BLOCK).  Synchronous. */
+kvr_status kvr_packed_bounds(const kvr_packed *packed, int32_t layer, int8_t *hi, int8_t *lo,
+                             float *unit);
+
+/* Query rows over packed documents: doc_rows[d] rows of document d, the rows of all
+ * documents one after another, each seeing the positions up to its own (-1: none,
+ * its output is zero).  positions: host int32, ascending within a document, below its
+ * length.  The handle keeps the tables that every layer's calls read; it holds no
+ * data of the documents.  kvr_rows_move gives the same rows new positions (a
+ * decoding step).  Both enqueue an upload and may allocate.  kvr_rows_free
+ * waits for the model's stream.  Errors: KVR_E_INVAL, KVR_E_RANGE, KVR_E_NOMEM. */
+kvr_status kvr_rows_create(kvr_model *model, kvr_packed *const *docs, const int32_t *doc_rows,
+                           int32_t n_docs, const int32_t *positions, kvr_rows **out);
+kvr_status kvr_rows_move(kvr_rows *rows, const int32_t *positions);
+void kvr_rows_free(kvr_rows *rows);
+
+/* Attention of layer `layer` of the rows over their documents: out[r][h] = sum_j
+ * softmax_j(q[r][h] . K[j] / sqrt(head_dim)) V[j] over j <= position of r, with
+ * the KV head of h / (n_heads / n_kv_heads).  q: rows [n_heads][head_dim] in the model
+ * dtype, ldq elements apart (at least n_heads * head_dim, a whole number of 16-byte
+ * pieces); out [rows][n_heads][head_dim], not overlapping q.  A row that sees a
+ * key or value row stored as NaN is NaN for that head; one that does not see it
+ * is untouched by it.  Errors: KVR_E_INVAL (a document freed since, pointers, ldq),
+ * KVR_E_RANGE (layer), KVR_E_POISONED, KVR_E_NOMEM. */
+kvr_status kvr_packed_attention(kvr_rows *rows, int32_t layer, const void *q, int32_t ldq,
+                                void *out);
+
+/* For each row and KV head the n_blocks blocks of KVR_BLOCK positions to attend to:
+ * the row's own (position / KVR_BLOCK) and, of those before it, the ones with the
+ * highest scores, ties to the lowest.  blocks_out [rows][n_kv_heads][n_blocks],
+ * ascending, -1 behind the last where the row sees fewer.  The score of block b is
+ * unit_b sum_c (P_c hi_bc + N_c lo_bc), P_c the sum over the group's query heads (in
+ * order, fp32) of max(q_c, 0) and N_c that of min(q_c, 0), both rounded to whole numbers of the
+ * smallest power of two t >= 2^-100 with every magnitude <= 127 t: an upper bound,
+ * up to those roundings, of the sum of the heads' largest products with a key of the
+ * block.  It is exact, so a choice does not depend on the order of sums.  Queries
+ * that are not finite score 0 everywhere.  Errors as kvr_packed_attention; KVR_E_RANGE
+ * for n_blocks outside [1, 16384]. */
+kvr_status kvr_packed_select(kvr_rows *rows, int32_t layer, const void *q, int32_t ldq,
+                             int32_t n_blocks, int32_t *blocks_out);
+
+/* kvr_packed_attention over the keys of the listed blocks alone (and j <= position):
+ * blocks [rows][n_kv_heads][n_blocks], in any order; entries below 0 or past the row's
+ * own block are passed over, one listed twice counts twice.  A row without a block
+ * is zero. */
+kvr_status kvr_packed_attention_blocks(kvr_rows *rows, int32_t layer, const void *q, int32_t ldq,
+                                       const int32_t *blocks, int32_t n_blocks, void *out);
+
 /* ---- inspection (tests, benchmarks) ---- */
 
 /* Number of cached positions n. */

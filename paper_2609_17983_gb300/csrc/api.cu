@@ -729,6 +729,7 @@ kvr_status sync_model(kvr_model *m, bool flag_queued = false) {
     cudaMemset(m->dev_flag, 0, sizeof(int));
     if (m->tcw.counters)
       cudaMemset(m->tcw.counters, 0, 2 * (size_t)m->tcw.max_tiles * sizeof(int));
+    if (m->pack_count) cudaMemset(m->pack_count, 0, m->pack_count_bytes);
     return fail(KVR_E_DEVICE_TIMEOUT, "a bounded device wait ran out (code %d)", flag);
   }
   return KVR_OK;
@@ -930,6 +931,18 @@ void dev_free(void *p) {
   else
     cudaFree(p);
 }
+
+kvr_status upload_words(kvr_model *m, void *dst, const void *src, size_t words) {
+  if (words <= m->stage_cap) return stage_h2d(m, (int32_t *)dst, (const int32_t *)src, words);
+  KVR_TRY(stage_flush(m));
+  CUDA_TRY(cudaMemcpyAsync(dst, src, words * 4, cudaMemcpyHostToDevice, m->stream));
+  return KVR_OK;
+}
+kvr_status grow_device(kvr_model *m, void *&buf, size_t &have, size_t need, const char *what) {
+  return grow_scratch(m, buf, have, need, what);
+}
+kvr_status synchronize(kvr_model *m) { return sync_model(m); }
+kvr_status flush_uploads(kvr_model *m) { return stage_flush(m); }
 }  // namespace kvr
 
 extern "C" {
@@ -952,6 +965,8 @@ void kvr_model_free(kvr_model *m) {
   cudaSetDevice(m->device);
   cudaStreamSynchronize(m->stream);
   while (!m->caches.empty()) kvr_cache_free(m->caches.back());
+  while (!m->rows.empty()) kvr_rows_free(m->rows.back());
+  while (!m->packed.empty()) kvr_packed_free(m->packed.back());
   trace_release(m);
   prof_collect(m);
   dev_free(m->weight_block);
@@ -972,6 +987,8 @@ void kvr_model_free(kvr_model *m) {
   dev_free(m->sel_scratch);
   dev_free(m->batch_scratch);
   dev_free(m->spare_pages);
+  dev_free(m->pack_ws);
+  dev_free(m->pack_count);
   dev_free(m->tcw.counters);
   dev_free(m->blocks_d);
   dev_free(m->attn_ws_o);

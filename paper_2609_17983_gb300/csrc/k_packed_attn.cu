@@ -1,0 +1,501 @@
+// k_packed_attn.cu -- attention over packed caches (packed.cuh): a few query vectors
+// against the 4-bit keys and values of their document, all of them up to the row's
+// position or those of listed blocks.
+//
+// A CTA owns a tile of up to eight query vectors (a row's heads of one KV head,
+// for several rows as many as fit) and a part of its pages; a warp takes every
+// WARPS-th page of the part by itself.  Per page, with keys as the rows of
+// m16n8k16 products (so that eight vectors fill one):
+//   S^T = K Q^T    the page's K half arrives in shared memory by one bulk copy, in
+//                  the order of the products' A fragments: a 16-byte load is four
+//                  fragments, each four conversions of two codes and four products with
+//                  the scales, which are exact in half;
+//   softmax        over the lane's own keys: the reference of a vector is raised only
+//                  when a score exceeds it by 8 in the log2 domain, so a page costs a
+//                  vote instead of a reduction; the sums stay apart until the end;
+//   O^T += V^T P^T P in half, its fragments transposed by movmatrix; V^T like K.
+// q is scaled by a power of two per vector so that it is a half as exactly as it
+// was a bf16; an fp32 model's q and P go as two halves each (22 bits), with
+// a page's products added to O in fp32 registers.  All sums are in fp32.
+// The warps' (max, sum, O) meet in shared memory, the parts' in the workspace, where the
+// last part to arrive adds them in order.
+//
+// A key whose row held a NaN or an infinity has NaN scales: its score is NaN for the
+// vectors that see it, and its V scales are cleared before the products, so
+// vectors that do not see it are untouched.
+#include <math.h>
+
+#include "packed.cuh"
+#include "tc_ptx.cuh"
+
+namespace kvr {
+namespace {
+using namespace ptx;
+
+constexpr int WARPS = 4;
+constexpr int STAGES = 2;           // pages in flight per warp
+constexpr float RAISE = 8.f;        // headroom of the reference (log2)
+constexpr float LIFT = 7.f;         // P = 2^(x - reference + LIFT) <= 2^15: more of a half's range
+constexpr int SPARSE_MAX = 128;     // listed blocks of a part
+
+// One contiguous copy into shared memory, counted at bar.
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes,
+                                          uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+          su32(dst)),
+      "l"(src), "r"(bytes), "r"(su32(bar))
+      : "memory");
+}
+
+// D (16 x 8, fp32) += A (16 x 16) B (16 x 8), halves.
+__device__ __forceinline__ void mma16816(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*(const __half2 *)&a, *(const __half2 *)&b);
+  return *(const uint32_t *)&r;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  const __half2 r = __floats2half2_rn(lo, hi);
+  return *(const uint32_t *)&r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Fragment of a K or V word: bytes 0 and 1 belong to scale s0, 2 and 3 to s1 (K: the
+// two keys), or bytes 0 and 2 to s0, 1 and 3 to s1 (V: the two pairs of keys).
+template <bool V>
+__device__ __forceinline__ void fragment(uint32_t w, uint32_t s0, uint32_t s1, uint32_t *a) {
+  a[0] = mul2(pack_values<0>(w), s0);
+  a[2] = mul2(pack_values<1>(w), V ? s1 : s0);
+  a[1] = mul2(pack_values<2>(w), V ? s0 : s1);
+  a[3] = mul2(pack_values<3>(w), s1);
+}
+
+// Four entries of a row of q.
+__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float *x) {
+  const uint2 u = *(const uint2 *)p;
+  x[0] = __uint_as_float(u.x << 16);
+  x[1] = __uint_as_float(u.x & 0xFFFF0000u);
+  x[2] = __uint_as_float(u.y << 16);
+  x[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void load4(const float *p, float *x) {
+  const float4 u = *(const float4 *)p;
+  x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+}
+__device__ __forceinline__ void store(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+__device__ __forceinline__ void store(float *p, float x) { *p = x; }
+
+// Weight of partial sums (m, l) under the common maximum M; NaN sums stay NaN.
+__device__ __forceinline__ float merge_weight(float m, float l, float M) {
+  return l != l ? l : m == -INFINITY ? 0.f : ex2(m - M);
+}
+
+template <int DH, typename T, bool SPARSE>
+__global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_attn(const PackedAttnArgs p) {
+  constexpr bool SPLIT = sizeof(T) == 4;
+  constexpr int HB = pack_half_bytes(DH), CB = pack_code_bytes(DH), DB = DH / 16, DQ = DH / 64;
+  extern __shared__ __align__(128) uint8_t smem[];  // [WARPS][STAGES][K half, V half]
+  __shared__ __align__(8) uint64_t full[WARPS][STAGES][2];
+  __shared__ float2 s_ml[WARPS][PACK_VEC];
+  __shared__ float s_wgt[WARPS][PACK_VEC];
+  __shared__ int s_list[SPARSE ? SPARSE_MAX : 1], s_count, s_last, abort_f;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lg = lane >> 2, lt = lane & 3;
+  const int g = blockIdx.y;
+  volatile int *abort_v = &abort_f;
+
+  if (lane == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full[warp][s][0], 1);
+      mbar_init(&full[warp][s][1], 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid == 0) abort_f = 0;
+  pdl_trigger();
+  pdl_wait();
+
+  // the tile, its part and pages
+  int vec0, nvec, doc, n_parts, part, slot, counter, n_pages;
+  int page0 = 0;
+  if (SPARSE) {
+    const int hc = (p.grp + PACK_VEC - 1) / PACK_VEC;  // chunks of a row's heads
+    const int tile = blockIdx.x / p.parts_per_row, row = tile / hc, h0 = tile % hc * PACK_VEC;
+    part = blockIdx.x % p.parts_per_row;
+    n_parts = p.parts_per_row;
+    vec0 = row * p.grp + h0;
+    nvec = min(PACK_VEC, p.grp - h0);
+    doc = p.row_doc[row];
+    slot = tile * n_parts;
+    counter = tile;
+    const int per = (p.n_blocks + n_parts - 1) / n_parts, i0 = part * per,
+              i1 = min(p.n_blocks, i0 + per);
+    const int pos = p.row_pos[row], own = pos < 0 ? -1 : pos / KVR_PAGE;
+    if (warp == 0) {
+      const int32_t *list = p.blocks + ((size_t)row * p.G + g) * p.n_blocks;
+      int n = 0;
+      for (int i = i0; i < i1; i += 32) {
+        const int b = i + lane < i1 ? list[i + lane] : -1;
+        const bool take = b >= 0 && b <= own;
+        const uint32_t m = __ballot_sync(0xFFFFFFFFu, take);
+        if (take) s_list[n + __popc(m & ((1u << lane) - 1))] = b;
+        n += __popc(m);
+      }
+      if (lane == 0) s_count = n;
+    }
+    __syncthreads();
+    n_pages = s_count;
+  } else {
+    const int4 pt = p.parts[blockIdx.x];
+    const PackedTile t = p.tiles[pt.x];
+    vec0 = t.vec0, nvec = t.nvec, doc = t.doc, n_parts = t.n_parts;
+    part = pt.w;
+    slot = t.part0;
+    counter = pt.x;
+    page0 = pt.y;
+    n_pages = pt.z - pt.y;
+    __syncthreads();
+  }
+  const PackedView v = p.docs[doc];
+  const uint8_t *blocks = v.block(p.layer, g, 0);
+  uint8_t *ring = smem + warp * (STAGES * 2 * HB);
+  const int n_my = n_pages > warp ? (n_pages - warp + WARPS - 1) / WARPS : 0;
+  auto page = [&](int i) {
+    const int at = warp + i * WARPS;
+    return SPARSE ? s_list[at] : page0 + at;
+  };
+  auto fetch = [&](int i, int kv) {  // one lane
+    uint64_t *bar = &full[warp][i % STAGES][kv];
+    mbar_expect_tx(bar, HB);
+    bulk_load(ring + (i % STAGES * 2 + kv) * HB,
+              blocks + (size_t)page(i) * (2 * HB) + kv * HB, HB, bar);
+  };
+  if (lane == 0)
+    for (int i = 0; i < min(n_my, STAGES); ++i) {
+      fetch(i, 0);
+      fetch(i, 1);
+    }
+
+  // q: this lane's vector lg, four entries of every 16
+  uint32_t qh[DB][2], ql[SPLIT ? DB : 1][2];
+  float qscale;  // of the products, into the log2 domain
+  {
+    float x[DB][4], a = 0.f;
+    const int vec = vec0 + lg;
+    const bool in = lg < nvec;
+    const T *q = (const T *)p.q + (size_t)(vec / p.grp) * p.ldq +
+                 (size_t)(g * p.grp + vec % p.grp) * DH + 4 * lt;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+      if (in)
+        load4(q + 16 * b, x[b]);
+      else
+        x[b][0] = x[b][1] = x[b][2] = x[b][3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a = fmaxf(a, fabsf(x[b][i]));
+    }
+    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+    a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+    // largest magnitude to [2^8, 2^9); what that leaves below a half's range is below
+    // 2^-32 of it
+    const int e = min(max((int)(__float_as_uint(a) >> 23) - 127, -100), 126) - 8;
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23),
+                upf = __uint_as_float((uint32_t)(127 + e) << 23);
+    qscale = upf * p.scale;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[b][i] *= down;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        qh[b][i] = half2_of(x[b][2 * i], x[b][2 * i + 1]);
+        if (SPLIT) {
+          const float2 f = __half22float2(*(const __half2 *)&qh[b][i]);
+          ql[b][i] = half2_of(x[b][2 * i] - f.x, x[b][2 * i + 1] - f.y);
+        }
+      }
+    }
+  }
+  // the vectors of this lane's columns of S^T and O^T: 2 lt and 2 lt + 1
+  float sc[2];
+  int pos[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    sc[c] = __shfl_sync(0xFFFFFFFFu, qscale, 4 * (2 * lt + c));
+    // a column without a vector is never masked: its results go nowhere
+    pos[c] = 2 * lt + c < nvec ? p.row_pos[(vec0 + 2 * lt + c) / p.grp] : 0x7FFFFFFF;
+  }
+  int least = min(pos[0], pos[1]);
+  least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, 1));
+  least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, 2));
+
+  float o[DB][4], ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int b = 0; b < DB; ++b) o[b][0] = o[b][1] = o[b][2] = o[b][3] = 0.f;
+
+  int done = 0;
+  for (; done < n_my; ++done) {
+    const int st = done % STAGES;
+    const uint8_t *kb = ring + st * 2 * HB, *vb = kb + HB;
+    bool ok = mbar_wait(&full[warp][st][0], done / STAGES & 1, abort_v, p.dev_flag, 1 << 12);
+    if (!__all_sync(0xFFFFFFFFu, ok)) break;
+    float s[4][4];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      s[kt][0] = s[kt][1] = s[kt][2] = s[kt][3] = 0.f;
+      uint32_t ks[2][DB / 4];  // scales of the two keys
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int b = 0; b < DB / 4; ++b)
+          ks[h][b] = *(const uint32_t *)(kb + CB + ((kt * 8 + lg) * 2 + h) * DB + 4 * b);
+#pragma unroll
+      for (int d4 = 0; d4 < DQ; ++d4) {
+        const uint4 w4 = *(const uint4 *)(kb + ((kt * DQ + d4) * 32 + lane) * 16);
+        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const uint32_t s0 = __byte_perm(ks[0][d4], 0, 0x4040 | b | b << 8) << 7,
+                         s1 = __byte_perm(ks[1][d4], 0, 0x4040 | b | b << 8) << 7;
+          uint32_t a[4];
+          fragment<false>(w[b], s0, s1, a);
+          mma16816(s[kt], a, qh[4 * d4 + b][0], qh[4 * d4 + b][1]);
+          if (SPLIT) mma16816(s[kt], a, ql[4 * d4 + b][0], ql[4 * d4 + b][1]);
+        }
+      }
+    }
+    const int first = page(done) * KVR_PAGE;
+    __syncwarp();
+    if (lane == 0 && done + STAGES < n_my) fetch(done + STAGES, 0);
+    ok = mbar_wait(&full[warp][st][1], done / STAGES & 1, abort_v, p.dev_flag, 1 << 13);
+    if (!__all_sync(0xFFFFFFFFu, ok)) break;
+    // scores; masked keys get none
+    float top[2] = {-INFINITY, -INFINITY};
+    // V rows marked NaN (all their scales): any byte of the first entries' scales
+    uint32_t nan[4];
+    {
+      const uint4 n4 = *(const uint4 *)(vb + CB + lt * 16);
+      nan[0] = __vcmpeq4(n4.x, 0xFFFFFFFFu);
+      nan[1] = __vcmpeq4(n4.y, 0xFFFFFFFFu);
+      nan[2] = __vcmpeq4(n4.z, 0xFFFFFFFFu);
+      nan[3] = __vcmpeq4(n4.w, 0xFFFFFFFFu);
+    }
+    const bool any_nan = __any_sync(0xFFFFFFFFu, (nan[0] | nan[1] | nan[2] | nan[3]) != 0);
+    if (any_nan) {
+      // their scores become NaN, their scales zero
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const uint32_t m = __shfl_sync(0xFFFFFFFFu, nan[kt], lg >> 1);  // keys 4 (lg / 2) .. + 3
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (m >> (8 * ((lg & 1) + 2 * h)) & 1) s[kt][2 * h] = s[kt][2 * h + 1] = NAN;
+      }
+      for (int i = lane; i < DB * 16; i += 32) {
+        uint32_t *x = (uint32_t *)(vb + CB) + i;
+        *x &= ~__vcmpeq4(*x, 0xFFFFFFFFu);
+      }
+      // before the copy that follows into this memory
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+    }
+    const bool masked = first + KVR_PAGE - 1 > least;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = i & 1, key = first + 16 * kt + pack_key_of(lg) + (i & 2);
+        s[kt][i] *= sc[c];
+        if (masked && key > pos[c]) s[kt][i] = -INFINITY;
+        top[c] = fmaxf(top[c], s[kt][i]);
+      }
+    if (__any_sync(0xFFFFFFFFu, top[0] > ref[0] + RAISE || top[1] > ref[1] + RAISE)) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2)
+          top[c] = fmaxf(top[c], __shfl_xor_sync(0xFFFFFFFFu, top[c], x));
+        const float now = fmaxf(ref[c], top[c]);
+        const float f = ref[c] == -INFINITY ? 0.f : ex2(ref[c] - now);
+        if (now > ref[c]) {  // sums so far are zero where there was no reference
+          l[c] = ref[c] == -INFINITY ? l[c] : l[c] * f;
+#pragma unroll
+          for (int b = 0; b < DB; ++b) {
+            if (ref[c] != -INFINITY) {
+              o[b][c] *= f;
+              o[b][c + 2] *= f;
+            }
+          }
+          ref[c] = now;
+        }
+      }
+    }
+    uint32_t ph[4][2], pl[SPLIT ? 4 : 1][2];  // fragments of P^T: 16 keys, lane's vector lg
+    {
+      const float base[2] = {(ref[0] == -INFINITY ? 0.f : ref[0]) - LIFT,
+                             (ref[1] == -INFINITY ? 0.f : ref[1]) - LIFT};
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float x = ex2(s[kt][2 * h] - base[0]), y = ex2(s[kt][2 * h + 1] - base[1]);
+          l[0] += x;
+          l[1] += y;
+          const uint32_t u = half2_of(x, y);
+          ph[kt][h] = transpose8x8(u);
+          if (SPLIT) {
+            const float2 f = __half22float2(*(const __half2 *)&u);
+            pl[kt][h] = transpose8x8(half2_of(x - f.x, y - f.y));
+          }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+      const uint4 w4 = *(const uint4 *)(vb + (b * 32 + (lane ^ b)) * 16);
+      const uint4 c4 = *(const uint4 *)(vb + CB + (b * 4 + lt) * 16);
+      const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w}, vs[4] = {c4.x, c4.y, c4.z, c4.w};
+      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      float *d = SPLIT ? acc : o[b];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const uint32_t s0 = __byte_perm(vs[kt], 0, 0x4140) << 7,
+                       s1 = __byte_perm(vs[kt], 0, 0x4342) << 7;
+        uint32_t a[4];
+        fragment<true>(w[kt], s0, s1, a);
+        mma16816(d, a, ph[kt][0], ph[kt][1]);
+        if (SPLIT) mma16816(d, a, pl[kt][0], pl[kt][1]);
+      }
+      if (SPLIT) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[b][i] += acc[i];
+      }
+    }
+    __syncwarp();
+    if (lane == 0 && done + STAGES < n_my) fetch(done + STAGES, 1);
+  }
+  // after a wait that ran out: the copies in flight end before the memory is reused
+  if (done < n_my)
+    for (int i = done; i < min(n_my, done + STAGES); ++i)
+      for (int kv = 0; kv < 2; ++kv)
+        mbar_wait(&full[warp][i % STAGES][kv], i / STAGES & 1, abort_v, p.dev_flag, 0, false);
+  __syncwarp();
+
+  // ---- the warps' sums ----
+  float *so = (float *)ring;  // [PACK_VEC][DH]
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int x = 4; x < 32; x *= 2) l[c] += __shfl_xor_sync(0xFFFFFFFFu, l[c], x);
+    if (lg == 0) s_ml[warp][2 * lt + c] = make_float2(ref[c], l[c]);
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+      so[(2 * lt + c) * DH + 16 * b + lg] = o[b][c];
+      so[(2 * lt + c) * DH + 16 * b + lg + 8] = o[b][c + 2];
+    }
+  }
+  __syncthreads();
+  __shared__ float2 s_tot[PACK_VEC];
+  if (tid < PACK_VEC) {
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) M = fmaxf(M, s_ml[w][tid].x);
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float2 ml = s_ml[w][tid];
+      const float f = merge_weight(ml.x, ml.y, M);
+      s_wgt[w][tid] = f;
+      L += f * ml.y;
+    }
+    s_tot[tid] = make_float2(M, L);
+  }
+  __syncthreads();
+  auto out_row = [&](int i) {  // vector i of the tile
+    const int vec = vec0 + i;
+    return (T *)p.out + ((size_t)(vec / p.grp) * p.H + g * p.grp + vec % p.grp) * DH;
+  };
+  const size_t at = ((size_t)(slot + part) * p.G + g) * PACK_VEC;
+  for (int i = tid; i < nvec * DH; i += WARPS * 32) {
+    const int vi = i / DH, d = i % DH;
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w)
+      x += s_wgt[w][vi] * ((const float *)(smem + w * (STAGES * 2 * HB)))[vi * DH + d];
+    if (n_parts == 1) {
+      const float L = s_tot[vi].y;
+      store(out_row(vi) + d, L == 0.f ? 0.f : x / L);  // no key: zeros
+    } else {
+      p.ws_o[at * DH + i] = x;
+    }
+  }
+  if (n_parts == 1) return;
+  if (tid < PACK_VEC) p.ws_ml[at + tid] = s_tot[tid];
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) s_last = atomicAdd(p.counters + (size_t)counter * p.G + g, 1) == n_parts - 1;
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  if (tid == 0) p.counters[(size_t)counter * p.G + g] = 0;
+  // ---- the last part adds them all, in order ----
+  const size_t at0 = ((size_t)slot * p.G + g) * PACK_VEC, step = (size_t)p.G * PACK_VEC;
+  for (int i = tid; i < nvec * DH; i += WARPS * 32) {
+    const int vi = i / DH, d = i % DH;
+    float M = -INFINITY, L = 0.f, x = 0.f;
+    for (int k = 0; k < n_parts; ++k) M = fmaxf(M, __ldcg(&p.ws_ml[at0 + k * step + vi].x));
+    for (int k = 0; k < n_parts; ++k) {
+      const float2 ml = __ldcg(&p.ws_ml[at0 + k * step + vi]);
+      const float f = merge_weight(ml.x, ml.y, M);
+      L += f * ml.y;
+      x += f * __ldcg(&p.ws_o[(at0 + k * step) * DH + i]);
+    }
+    store(out_row(vi) + d, L == 0.f ? 0.f : x / L);
+  }
+}
+
+PerDevice<size_t> attn_smem[8];
+
+}  // namespace
+
+int packed_attn_warps() { return WARPS; }
+int packed_attn_ctas_per_sm(int dtype) { return dtype == KVR_DTYPE_BF16 ? 3 : 2; }
+int packed_attn_max_blocks_per_part() { return SPARSE_MAX; }
+size_t packed_attn_ws_floats(int n_parts, int G, int dh) {
+  return (size_t)n_parts * G * PACK_VEC * dh;
+}
+
+const char *launch_packed_attention(const PackedAttnArgs &a, cudaStream_t s) {
+  const size_t smem = (size_t)WARPS * STAGES * pack_block_bytes(a.dh);
+  const int hc = (a.grp + PACK_VEC - 1) / PACK_VEC;
+  const dim3 grid(a.blocks ? a.n_rows * hc * a.parts_per_row : a.n_parts, a.G);
+  auto run = [&](auto kernel, int which) -> const char * {
+    if (const char *e = smem_opt_in(attn_smem[which], kernel, smem)) return e;
+    const cudaError_t e = launch_pdl(kernel, grid, dim3(WARPS * 32), smem, s, a);
+    return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+  };
+  using B = __nv_bfloat16;
+  if (a.blocks) {
+    if (a.dtype == KVR_DTYPE_BF16)
+      return a.dh == 128 ? run(k_packed_attn<128, B, true>, 0) : run(k_packed_attn<64, B, true>, 1);
+    return a.dh == 128 ? run(k_packed_attn<128, float, true>, 2)
+                       : run(k_packed_attn<64, float, true>, 3);
+  }
+  if (a.dtype == KVR_DTYPE_BF16)
+    return a.dh == 128 ? run(k_packed_attn<128, B, false>, 4) : run(k_packed_attn<64, B, false>, 5);
+  return a.dh == 128 ? run(k_packed_attn<128, float, false>, 6)
+                     : run(k_packed_attn<64, float, false>, 7);
+}
+
+}  // namespace kvr

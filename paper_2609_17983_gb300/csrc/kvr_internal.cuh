@@ -221,10 +221,14 @@ struct ProfClass {
 }  // namespace kvr
 
 struct kvr_cache;
+struct kvr_packed;
+struct kvr_rows;
 
 struct kvr_model {
   kvr::Dims dims{};
   std::vector<kvr_cache *> caches;  // live caches, freed with the model
+  std::vector<kvr_packed *> packed;  // live packed caches and rows over them, likewise
+  std::vector<kvr_rows *> rows;
   void *weight_block = nullptr;
   size_t weight_bytes = 0;
   void *embed = nullptr, *lm_head = nullptr;
@@ -271,6 +275,10 @@ struct kvr_model {
   void *spare_pages = nullptr;
   size_t spare_bytes = 0;
   CUtensorMap tm_spare;  // their TMA view
+  void *pack_ws = nullptr;     // packed attention: partial sums of split tiles
+  size_t pack_ws_bytes = 0;
+  void *pack_count = nullptr;  // and their arrivals, zero between calls
+  size_t pack_count_bytes = 0;
   int *dev_flag = nullptr;     // device error flag (bounded waits)
   kvr::TraceBuf trace{};       // attached device timeline buffer, if any
   kvr::SplitView pending{};    // split tiles of h not yet added (next RMSNorm adds them)

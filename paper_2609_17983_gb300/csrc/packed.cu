@@ -1,0 +1,462 @@
+// packed.cu -- the packed cache's entry points: documents held in 4 bits, their rows
+// written and read back, and query rows that attend to them.
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+
+#include "packed.cuh"
+
+using namespace kvr;
+
+namespace {
+
+constexpr int MAX_CAPACITY = 1 << 20;  // positions of a packed cache
+constexpr int MAX_ROWS = 1 << 20, MAX_DOCS = 4096, MAX_BLOCKS = MAX_CAPACITY / KVR_PAGE;
+
+kvr_status fail(kvr_status code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  set_last_error(buf);
+  return code;
+}
+
+#define KVR_TRY(expr)              \
+  do {                             \
+    kvr_status s__ = (expr);       \
+    if (s__ != KVR_OK) return s__; \
+  } while (0)
+
+kvr_status use_device(const kvr_model *m) {
+  const cudaError_t e = cudaSetDevice(m->device);
+  return e == cudaSuccess ? KVR_OK : fail(KVR_E_CUDA, "cudaSetDevice: %s", cudaGetErrorString(e));
+}
+
+kvr_status launched(kvr_model *m, int kernels, const char *what) {
+  m->launches += kernels;
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? KVR_OK : fail(KVR_E_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// Device or managed memory that `device` can use, on a 16-byte boundary.
+kvr_status check_device_ptr(const kvr_model *m, const void *p, const char *name) {
+  if (!p) return fail(KVR_E_INVAL, "NULL %s", name);
+  if ((uintptr_t)p & 15) return fail(KVR_E_INVAL, "%s is not 16-byte aligned", name);
+  cudaPointerAttributes a{};
+  if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
+    cudaGetLastError();
+    return fail(KVR_E_INVAL, "%s is not device memory", name);
+  }
+  if (a.type == cudaMemoryTypeManaged || (a.type == cudaMemoryTypeDevice && a.device == m->device))
+    return KVR_OK;
+  return fail(KVR_E_INVAL, "%s is not memory of the model's device", name);
+}
+
+// Positions of a call (ascending) in segments of a page each; many scattered ones go to
+// the model's readback scratch.
+kvr_status rows_of(kvr_model *m, const int32_t *pos, int n, PackedRows &r) {
+  r.n = n;
+  if (pos[n - 1] - pos[0] == n - 1) {
+    r.first = pos[0];
+    r.n_seg = pos[n - 1] / KVR_PAGE - pos[0] / KVR_PAGE + 1;
+    return KVR_OK;
+  }
+  std::vector<int32_t> seg;
+  for (int i = 0; i < n; ++i)
+    if (!i || pos[i] / KVR_PAGE != pos[i - 1] / KVR_PAGE) seg.push_back(i);
+  r.n_seg = (int)seg.size();
+  seg.push_back(n);
+  if (n <= PACK_INLINE_POS) {
+    for (size_t i = 0; i < seg.size(); ++i) r.seg[i] = (uint16_t)seg[i];
+    memcpy(r.pos, pos, n * sizeof(int32_t));
+    return KVR_OK;
+  }
+  std::vector<int32_t> all(pos, pos + n);
+  all.insert(all.end(), seg.begin(), seg.end());
+  KVR_TRY(grow_device(m, m->read_scratch, m->read_scratch_bytes, all.size() * 4,
+                      "readback scratch"));
+  KVR_TRY(upload_words(m, m->read_scratch, all.data(), all.size()));
+  r.pos_d = (const int32_t *)m->read_scratch;
+  return KVR_OK;
+}
+
+kvr_status check_range(const kvr_model *m, const int32_t *positions, int n, int l0, int l1,
+                       int end) {
+  if (n < 0) return fail(KVR_E_RANGE, "negative number of positions");
+  if (l0 < 0 || l1 > m->dims.L || l0 > l1)
+    return fail(KVR_E_RANGE, "layers [%d, %d) outside [0, %d)", l0, l1, m->dims.L);
+  if (n > 0 && !positions) return fail(KVR_E_INVAL, "NULL positions");
+  for (int i = 0; i < n; ++i) {
+    if (positions[i] < 0 || positions[i] >= end)
+      return fail(KVR_E_RANGE, "position %d outside [0, %d)", positions[i], end);
+    if (i && positions[i] <= positions[i - 1])
+      return fail(KVR_E_RANGE, "positions not strictly increasing at %d", i);
+  }
+  return KVR_OK;
+}
+
+// ------------------------------------------------------------ query rows
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+kvr_status check_rows(const std::vector<kvr_packed *> &docs, const std::vector<int32_t> &doc_rows,
+                      const int32_t *pos, size_t count) {
+  size_t i = 0;
+  for (size_t d = 0; d < docs.size(); ++d)
+    for (int r = 0; r < doc_rows[d]; ++r, ++i) {
+      if (pos[i] < -1 || pos[i] >= docs[d]->n)
+        return fail(KVR_E_RANGE, "row %zu: position %d outside [-1, %d)", i, pos[i], docs[d]->n);
+      if (r && pos[i] < pos[i - 1])
+        return fail(KVR_E_RANGE, "row %zu: positions of a document descend", i);
+    }
+  return i == count ? KVR_OK : fail(KVR_E_RANGE, "row counts do not match");
+}
+
+// The tables of rows at `pos`, built and sent.
+kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
+  kvr_model *m = r->model;
+  const Dims &dm = m->dims;
+  const int grp = dm.H / dm.G, M = (int)r->pos.size(), D = (int)r->docs.size();
+  std::vector<PackedTile> tiles;
+  std::vector<int> pages;  // of a tile
+  std::vector<int32_t> doc(M);
+  long long total = 0;
+  int row0 = 0, most = 1;
+  for (int d = 0; d < D; ++d) {
+    const int R = r->doc_rows[d];
+    std::fill(doc.begin() + row0, doc.begin() + row0 + R, d);
+    for (int v = 0; v < R * grp; v += PACK_VEC) {
+      PackedTile t{};
+      t.vec0 = row0 * grp + v;
+      t.nvec = std::min(PACK_VEC, R * grp - v);
+      t.doc = d;
+      const int last = pos[(t.vec0 + t.nvec - 1) / grp];  // positions ascend
+      const int np = last < 0 ? 0 : last / KVR_PAGE + 1;
+      tiles.push_back(t);
+      pages.push_back(np);
+      total += np;
+      most = std::max(most, np);
+    }
+    row0 += R;
+  }
+  // parts of whole rounds of the warps, as many as fill the chip once
+  const int W = packed_attn_warps();
+  const long long slots = std::max(1, m->num_sms * packed_attn_ctas_per_sm(dm.dtype) / dm.G);
+  const int per = (int)std::max<long long>(1, ((total + slots - 1) / slots + W - 1) / W) * W;
+  std::vector<int4> parts;
+  for (size_t t = 0; t < tiles.size(); ++t) {
+    tiles[t].part0 = (int)parts.size();
+    tiles[t].n_parts = std::max(1, (pages[t] + per - 1) / per);
+    for (int k = 0; k < tiles[t].n_parts; ++k)
+      parts.push_back(make_int4((int)t, std::min(pages[t], k * per),
+                                std::min(pages[t], (k + 1) * per), k));
+  }
+  const size_t o_doc = 0, o_tile = up256(o_doc + D * sizeof(PackedView)),
+               o_part = up256(o_tile + tiles.size() * sizeof(PackedTile)),
+               o_pos = up256(o_part + parts.size() * sizeof(int4)), o_rd = up256(o_pos + M * 4ull),
+               bytes = up256(o_rd + M * 4ull);
+  std::vector<char> host(bytes);
+  for (int d = 0; d < D; ++d) {
+    const PackedView v = r->docs[d]->view();
+    memcpy(host.data() + o_doc + d * sizeof v, &v, sizeof v);
+  }
+  memcpy(host.data() + o_tile, tiles.data(), tiles.size() * sizeof(PackedTile));
+  memcpy(host.data() + o_part, parts.data(), parts.size() * sizeof(int4));
+  memcpy(host.data() + o_pos, pos, M * 4ull);
+  memcpy(host.data() + o_rd, doc.data(), M * 4ull);
+  r->docs_d = nullptr;  // no tables until they are sent
+  KVR_TRY(grow_device(m, r->mem, r->mem_bytes, bytes, "query rows"));
+  KVR_TRY(upload_words(m, r->mem, host.data(), bytes / 4));
+  char *base = (char *)r->mem;
+  r->docs_d = (PackedView *)(base + o_doc);
+  r->tiles_d = (PackedTile *)(base + o_tile);
+  r->parts_d = (int4 *)(base + o_part);
+  r->pos_d = (int32_t *)(base + o_pos);
+  r->doc_d = (int32_t *)(base + o_rd);
+  r->n_parts = (int)parts.size();
+  r->n_tiles = (int)tiles.size();
+  r->max_pages = most;
+  std::copy(pos, pos + M, r->pos.begin());
+  return KVR_OK;
+}
+
+// Room for the partial sums and arrival counts of a launch.
+kvr_status attn_workspace(kvr_model *m, PackedAttnArgs &a, long long parts, long long tiles) {
+  const size_t o = up256(packed_attn_ws_floats((int)parts, a.G, a.dh) * 4),
+               ml = (size_t)parts * a.G * PACK_VEC * sizeof(float2), cb = (size_t)tiles * a.G * 4;
+  if (o + ml > m->pack_ws_bytes)
+    KVR_TRY(grow_device(m, m->pack_ws, m->pack_ws_bytes, o + ml, "packed attention workspace"));
+  if (cb > m->pack_count_bytes) {
+    KVR_TRY(grow_device(m, m->pack_count, m->pack_count_bytes, cb, "packed attention counters"));
+    if (cudaMemsetAsync(m->pack_count, 0, cb, m->stream) != cudaSuccess)
+      return fail(KVR_E_CUDA, "packed attention counters");
+  }
+  a.ws_o = (float *)m->pack_ws;
+  a.ws_ml = (float2 *)((char *)m->pack_ws + o);
+  a.counters = (int *)m->pack_count;
+  return KVR_OK;
+}
+
+// Checks common to the calls on rows, and what their kernels take.
+kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, PackedAttnArgs &a) {
+  if (!r) return fail(KVR_E_INVAL, "NULL rows");
+  kvr_model *m = r->model;
+  const Dims &dm = m->dims;
+  if (layer < 0 || layer >= dm.L) return fail(KVR_E_RANGE, "layer %d outside [0, %d)", layer, dm.L);
+  for (const kvr_packed *d : r->docs) {
+    if (!d) return fail(KVR_E_INVAL, "a document of these rows has been freed");
+    if (d->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned");
+  }
+  if (!r->docs_d) return fail(KVR_E_INVAL, "rows whose last move failed");
+  if (ldq < dm.H * dm.dh || ldq * dm.es() % 16)
+    return fail(KVR_E_INVAL, "row stride %d of q: at least %d, whole 16-byte pieces", ldq,
+                dm.H * dm.dh);
+  KVR_TRY(use_device(m));
+  KVR_TRY(check_device_ptr(m, q, "q"));
+  a = PackedAttnArgs{};
+  a.q = q;
+  a.ldq = ldq;
+  a.dtype = dm.dtype;
+  a.H = dm.H, a.G = dm.G, a.grp = dm.H / dm.G, a.dh = dm.dh;
+  a.layer = layer;
+  a.scale = (float)(1.4426950408889634 / std::sqrt((double)dm.dh));
+  a.docs = r->docs_d;
+  a.row_pos = r->pos_d;
+  a.row_doc = r->doc_d;
+  a.tiles = r->tiles_d;
+  a.parts = r->parts_d;
+  a.n_parts = r->n_parts;
+  a.n_rows = (int)r->pos.size();
+  a.dev_flag = m->dev_flag;
+  return KVR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+kvr_status kvr_packed_create(kvr_model *m, int32_t capacity, kvr_packed **out) {
+  if (!m || !out) return fail(KVR_E_INVAL, "NULL argument");
+  *out = nullptr;
+  if (capacity < 1 || capacity > MAX_CAPACITY)
+    return fail(KVR_E_RANGE, "capacity %d outside [1, %d]", capacity, MAX_CAPACITY);
+  KVR_TRY(use_device(m));
+  const Dims &dm = m->dims;
+  kvr_packed *c = new kvr_packed();
+  c->model = m;
+  c->cap = capacity;
+  c->pages = (capacity + KVR_PAGE - 1) / KVR_PAGE;
+  const size_t n = (size_t)dm.L * dm.G * c->pages, block_b = n * pack_block_bytes(dm.dh),
+               bound_b = n * 2 * dm.dh;
+  c->blocks = (uint8_t *)dev_alloc(block_b);
+  c->bounds = (int8_t *)dev_alloc(bound_b);
+  c->unit = (float *)dev_alloc(n * sizeof(float));
+  m->packed.push_back(c);
+  if (!c->blocks || !c->bounds || !c->unit) {
+    kvr_packed_free(c);
+    return fail(KVR_E_NOMEM, "packed cache of %d positions", capacity);
+  }
+  if (cudaMemsetAsync(c->blocks, 0, block_b, m->stream) != cudaSuccess ||
+      cudaMemsetAsync(c->bounds, 0, bound_b, m->stream) != cudaSuccess ||
+      cudaMemsetAsync(c->unit, 0, n * sizeof(float), m->stream) != cudaSuccess) {
+    kvr_packed_free(c);
+    return fail(KVR_E_CUDA, "packed cache clear");
+  }
+  *out = c;
+  return KVR_OK;
+}
+
+void kvr_packed_free(kvr_packed *c) {
+  if (!c) return;
+  kvr_model *m = c->model;
+  cudaSetDevice(m->device);
+  flush_uploads(m);
+  cudaStreamSynchronize(m->stream);
+  m->packed.erase(std::remove(m->packed.begin(), m->packed.end(), c), m->packed.end());
+  for (kvr_rows *r : m->rows) std::replace(r->docs.begin(), r->docs.end(), c, (kvr_packed *)nullptr);
+  dev_free(c->blocks);
+  dev_free(c->bounds);
+  dev_free(c->unit);
+  delete c;
+}
+
+int32_t kvr_packed_len(const kvr_packed *c) { return c ? c->n : -1; }
+
+kvr_status kvr_packed_write(kvr_packed *c, const int32_t *positions, int32_t n_pos, int32_t l0,
+                            int32_t l1, const void *k, const void *v) {
+  if (!c) return fail(KVR_E_INVAL, "NULL packed cache");
+  if (c->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned by an earlier CUDA error");
+  kvr_model *m = c->model;
+  KVR_TRY(check_range(m, positions, n_pos, l0, l1, c->cap));
+  for (int i = 0, end = c->n; i < n_pos; ++i) {
+    if (positions[i] > end)
+      return fail(KVR_E_RANGE, "position %d leaves a gap after %d", positions[i], end);
+    end = std::max(end, positions[i] + 1);
+  }
+  if (n_pos == 0 || l0 == l1) return KVR_OK;
+  KVR_TRY(use_device(m));
+  KVR_TRY(check_device_ptr(m, k, "k"));
+  KVR_TRY(check_device_ptr(m, v, "v"));
+  PackedRows rows;
+  KVR_TRY(rows_of(m, positions, n_pos, rows));
+  const int len = std::max(c->n, positions[n_pos - 1] + 1);
+  launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->stream);
+  const kvr_status st = launched(m, 1, "packed write");
+  if (st)
+    c->poisoned = true;
+  else
+    c->n = len;
+  return st;
+}
+
+kvr_status kvr_packed_read(const kvr_packed *c, const int32_t *positions, int32_t n_pos,
+                           int32_t l0, int32_t l1, void *k_out, void *v_out) {
+  if (!c) return fail(KVR_E_INVAL, "NULL packed cache");
+  if (c->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned");
+  kvr_model *m = c->model;
+  KVR_TRY(check_range(m, positions, n_pos, l0, l1, c->n));
+  if (n_pos == 0 || l0 == l1) return KVR_OK;
+  KVR_TRY(use_device(m));
+  KVR_TRY(check_device_ptr(m, k_out, "k_out"));
+  KVR_TRY(check_device_ptr(m, v_out, "v_out"));
+  PackedRows rows;
+  KVR_TRY(rows_of(m, positions, n_pos, rows));
+  launch_packed_read(c->view(), m->dims.dtype, rows, l0, l1 - l0, k_out, v_out, m->stream);
+  return launched(m, 1, "packed read");
+}
+
+kvr_status kvr_packed_bounds(const kvr_packed *c, int32_t layer, int8_t *hi, int8_t *lo,
+                             float *unit) {
+  if (!c || !hi || !lo || !unit) return fail(KVR_E_INVAL, "NULL argument");
+  kvr_model *m = c->model;
+  const Dims &dm = m->dims;
+  if (layer < 0 || layer >= dm.L) return fail(KVR_E_RANGE, "layer %d outside [0, %d)", layer, dm.L);
+  KVR_TRY(use_device(m));
+  KVR_TRY(synchronize(m));
+  const int used = (c->n + KVR_PAGE - 1) / KVR_PAGE;
+  const PackedView v = c->view();
+  std::vector<int8_t> both((size_t)used * 2 * dm.dh);
+  for (int g = 0; g < dm.G && used; ++g) {
+    const size_t at = v.index(layer, g, 0);
+    if (cudaMemcpy(both.data(), v.bounds + at * 2 * dm.dh, both.size(), cudaMemcpyDeviceToHost) !=
+            cudaSuccess ||
+        cudaMemcpy(unit + (size_t)g * used, v.unit + at, used * sizeof(float),
+                   cudaMemcpyDeviceToHost) != cudaSuccess)
+      return fail(KVR_E_CUDA, "bounds readback");
+    for (int b = 0; b < used; ++b) {
+      memcpy(hi + ((size_t)g * used + b) * dm.dh, both.data() + (size_t)b * 2 * dm.dh, dm.dh);
+      memcpy(lo + ((size_t)g * used + b) * dm.dh, both.data() + (size_t)(b * 2 + 1) * dm.dh, dm.dh);
+    }
+  }
+  return KVR_OK;
+}
+
+kvr_status kvr_rows_create(kvr_model *m, kvr_packed *const *docs, const int32_t *doc_rows,
+                           int32_t n_docs, const int32_t *positions, kvr_rows **out) {
+  if (!m || !docs || !doc_rows || !positions || !out) return fail(KVR_E_INVAL, "NULL argument");
+  *out = nullptr;
+  if (n_docs < 1 || n_docs > MAX_DOCS)
+    return fail(KVR_E_RANGE, "n_docs=%d outside [1, %d]", n_docs, MAX_DOCS);
+  long long M = 0;
+  for (int d = 0; d < n_docs; ++d) {
+    if (!docs[d] || docs[d]->model != m) return fail(KVR_E_INVAL, "document %d: bad handle", d);
+    if (doc_rows[d] < 0) return fail(KVR_E_RANGE, "document %d: negative rows", d);
+    M += doc_rows[d];
+  }
+  if (M < 1 || M > MAX_ROWS) return fail(KVR_E_RANGE, "%lld rows outside [1, %d]", M, MAX_ROWS);
+  std::vector<kvr_packed *> dv(docs, docs + n_docs);
+  std::vector<int32_t> rv(doc_rows, doc_rows + n_docs);
+  KVR_TRY(check_rows(dv, rv, positions, (size_t)M));
+  KVR_TRY(use_device(m));
+  kvr_rows *r = new kvr_rows();
+  r->model = m;
+  r->docs = std::move(dv);
+  r->doc_rows = std::move(rv);
+  r->pos.resize(M);
+  m->rows.push_back(r);
+  if (const kvr_status st = build_rows(r, positions)) {
+    kvr_rows_free(r);
+    return st;
+  }
+  *out = r;
+  return KVR_OK;
+}
+
+kvr_status kvr_rows_move(kvr_rows *r, const int32_t *positions) {
+  if (!r || !positions) return fail(KVR_E_INVAL, "NULL argument");
+  for (const kvr_packed *d : r->docs)
+    if (!d) return fail(KVR_E_INVAL, "a document of these rows has been freed");
+  KVR_TRY(check_rows(r->docs, r->doc_rows, positions, r->pos.size()));
+  KVR_TRY(use_device(r->model));
+  return build_rows(r, positions);
+}
+
+void kvr_rows_free(kvr_rows *r) {
+  if (!r) return;
+  kvr_model *m = r->model;
+  cudaSetDevice(m->device);
+  flush_uploads(m);
+  cudaStreamSynchronize(m->stream);
+  m->rows.erase(std::remove(m->rows.begin(), m->rows.end(), r), m->rows.end());
+  dev_free(r->mem);
+  delete r;
+}
+
+kvr_status kvr_packed_attention(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, void *out) {
+  PackedAttnArgs a;
+  KVR_TRY(rows_args(r, layer, q, ldq, a));
+  kvr_model *m = r->model;
+  KVR_TRY(check_device_ptr(m, out, "out"));
+  a.out = out;
+  KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles));
+  if (const char *e = launch_packed_attention(a, m->stream))
+    return fail(KVR_E_CUDA, "packed attention: %s", e);
+  return launched(m, 1, "packed attention");
+}
+
+kvr_status kvr_packed_select(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
+                             int32_t n_blocks, int32_t *blocks_out) {
+  PackedAttnArgs a;
+  KVR_TRY(rows_args(r, layer, q, ldq, a));
+  if (n_blocks < 1 || n_blocks > MAX_BLOCKS)
+    return fail(KVR_E_RANGE, "n_blocks=%d outside [1, %d]", n_blocks, MAX_BLOCKS);
+  kvr_model *m = r->model;
+  KVR_TRY(check_device_ptr(m, blocks_out, "blocks_out"));
+  a.n_blocks = n_blocks;
+  if (const char *e = launch_packed_select(a, r->max_pages, blocks_out, m->stream))
+    return fail(KVR_E_CUDA, "block selection: %s", e);
+  return launched(m, 1, "block selection");
+}
+
+kvr_status kvr_packed_attention_blocks(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
+                                       const int32_t *blocks, int32_t n_blocks, void *out) {
+  PackedAttnArgs a;
+  KVR_TRY(rows_args(r, layer, q, ldq, a));
+  if (n_blocks < 1 || n_blocks > MAX_BLOCKS)
+    return fail(KVR_E_RANGE, "n_blocks=%d outside [1, %d]", n_blocks, MAX_BLOCKS);
+  kvr_model *m = r->model;
+  KVR_TRY(check_device_ptr(m, out, "out"));
+  KVR_TRY(check_device_ptr(m, blocks, "blocks"));
+  a.out = out;
+  a.blocks = blocks;
+  a.n_blocks = n_blocks;
+  // parts of whole rounds of the warps, as many as fill the chip once
+  const int W = packed_attn_warps(), most = packed_attn_max_blocks_per_part();
+  const long long tiles = (long long)a.n_rows * ((a.grp + PACK_VEC - 1) / PACK_VEC);
+  const long long slots = (long long)m->num_sms * packed_attn_ctas_per_sm(a.dtype);
+  const long long each = (tiles * a.G * n_blocks + slots - 1) / slots;
+  const int per = (int)std::min<long long>(most, std::max<long long>(1, (each + W - 1) / W) * W);
+  a.parts_per_row = (n_blocks + per - 1) / per;
+  if (tiles * a.parts_per_row > 0x7FFFFFFF)
+    return fail(KVR_E_UNSUPPORTED, "too many rows (%d) for %d blocks each", a.n_rows, n_blocks);
+  KVR_TRY(attn_workspace(m, a, tiles * a.parts_per_row, tiles));
+  if (const char *e = launch_packed_attention(a, m->stream))
+    return fail(KVR_E_CUDA, "block attention: %s", e);
+  return launched(m, 1, "block attention");
+}
+
+}  // extern "C"

@@ -1,0 +1,208 @@
+// packed.cuh -- a document's K/V in 4 bits: the stored form and its device helpers.
+//
+// Values.  Groups of 16 consecutive entries of head_dim share a scale.  With a the
+// group's largest magnitude, s = a / 6 rounded to 5 exponent and 3 mantissa bits (to
+// nearest, ties to even; at most PACK_MAX_SCALE): a half without its sign and low
+// seven bits, so its bits are the code << 7.  An entry's code is x / s rounded (to nearest,
+// ties to the even code) to one of {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign, saturating.
+// The value code * s has at most six significant bits: exact in half, bf16 and float.
+// A row (position, KV head, K or V) that holds a NaN or an infinity has the scale code
+// PACK_NAN throughout and reads back as NaN.
+//
+// Layout.  64 positions (a page) of one layer and KV head are one block of 72 * dh
+// bytes; blocks lie [layer][kv head][page].  A block is K codes, K scales, V codes,
+// V scales, in the order in which a warp's m16n8k16 products take them: with lane =
+// 4 g + t, tile kt of 16 keys and tile db of 16 entries,
+//   K codes   [kt][db / 4][lane][db % 4] 32-bit words: low half-word the four entries
+//             db*16 + 4t .. of key kt*16 + key_of(g), high half-word those of the key
+//             two further; entry i in bits 4i .. 4i + 3;
+//   K scales  [kt][g][high][db] bytes;
+//   V codes   [db][lane ^ db][kt] words: low half-word the four keys kt*16 + 4t .. of entry
+//             db*16 + g, high half-word those of entry db*16 + g + 8 (lane ^ db: the
+//             units of a column of db's lie in different banks for kernels that
+//             take a row apart);
+//   V scales  [db][t][kt][j] bytes, j the key of the four.
+// Slots that nothing wrote are zero (scale 0, value 0).
+//
+// Bounds.  Per block the largest and the least value of each key entry over the
+// finite rows present, as whole numbers hi = ceil(max / u), lo = floor(min / u) of
+// the smallest power of two u with every magnitude <= 127 u: [layer][kv head][page][hi, lo][dh]
+// bytes, and u (float) [layer][kv head][page].
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "kvr_internal.cuh"
+
+namespace kvr {
+
+constexpr int PACK_GROUP = 16;
+constexpr int PACK_NAN = 0xFF;
+constexpr int PACK_MAX_CODE = 0xE2;         // the scale 10240: 6 * 10240 is still a half
+constexpr float PACK_MAX_SCALE = 10240.f;
+
+__host__ __device__ constexpr int pack_half_bytes(int dh) { return 36 * dh; }  // K or V of a block
+__host__ __device__ constexpr int pack_code_bytes(int dh) { return 32 * dh; }
+__host__ __device__ constexpr int pack_block_bytes(int dh) { return 72 * dh; }
+
+// Key (of a tile of 16) whose entries are the low half-words of lanes 4g .. 4g + 3.
+__host__ __device__ constexpr int pack_key_of(int g) { return 4 * (g >> 1) + (g & 1); }
+
+// Byte offsets within a block's K half: the half-word of (key, entries e4 .. e4 + 3),
+// and the scale of (key, db).
+__host__ __device__ inline int pack_k_code(int dh, int key, int e4) {
+  const int kt = key >> 4, r = key & 15, g = 2 * (r >> 2) + (r & 1), hi = (r >> 1) & 1;
+  const int db = e4 >> 4, t = (e4 & 15) >> 2;
+  return (((kt * (dh / 64) + (db >> 2)) * 32 + 4 * g + t) * 4 + (db & 3)) * 4 + 2 * hi;
+}
+__host__ __device__ inline int pack_k_scale(int dh, int key, int db) {
+  const int kt = key >> 4, r = key & 15, g = 2 * (r >> 2) + (r & 1), hi = (r >> 1) & 1;
+  return pack_code_bytes(dh) + ((kt * 8 + g) * 2 + hi) * (dh / 16) + db;
+}
+// Within the V half: the half-word of (keys 4 * key4 .. + 3, entry), and the scale
+// of (key, db).
+__host__ __device__ inline int pack_v_code(int key4, int entry) {
+  const int db = entry >> 4, r = entry & 15, lane = 4 * (r & 7) + (key4 & 3);
+  return ((db * 32 + (lane ^ db)) * 4 + (key4 >> 2)) * 4 + 2 * (r >> 3);
+}
+__host__ __device__ inline int pack_v_scale(int dh, int key, int db) {
+  return pack_code_bytes(dh) + ((db * 4 + ((key & 15) >> 2)) * 4 + (key >> 4)) * 4 + (key & 3);
+}
+
+// Device view of one packed document.
+struct PackedView {
+  uint8_t *blocks;
+  int8_t *bounds;
+  float *unit;
+  int pages;  // capacity
+  int G, dh;
+  __host__ __device__ size_t index(int layer, int g, int page) const {
+    return ((size_t)layer * G + g) * pages + page;
+  }
+  __host__ __device__ uint8_t *block(int layer, int g, int page) const {
+    return blocks + index(layer, g, page) * pack_block_bytes(dh);
+  }
+};
+
+// The half2 of two codes in a byte of w (low nibble first).
+template <int BYTE>
+__device__ __forceinline__ uint32_t pack_values(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 b;\n\t.reg .b32 t;\n\tshr.b32 t, %1, %2;\n\tcvt.u8.u32 b, t;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b;\n\t}"
+      : "=r"(r)
+      : "r"(w), "n"(8 * BYTE));
+  return r;
+}
+
+// Codes of a (low nibble) and b.
+__device__ __forceinline__ uint32_t pack_codes(float a, float b) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %2, %1;\n\tcvt.u32.u8 %0, c;\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b));
+  return r;
+}
+
+// Scale of a group whose largest magnitude is a (finite), as its code.  The rounding to
+// three mantissa bits is a float's own: above 2^-14 of the mantissa's bits, below in
+// whole steps of 2^-17.
+__device__ __forceinline__ uint32_t pack_scale_code(float a) {
+  const float s = fminf(__fdiv_rn(a, 6.f), PACK_MAX_SCALE);
+  if (s < 6.103515625e-05f) return (uint32_t)__float2int_rn(s * 131072.f);  // 2^-14, 2^17
+  uint32_t u = __float_as_uint(s);
+  u = (u + 0x7FFFFu + ((u >> 20) & 1u)) >> 20;  // exponent and three mantissa bits
+  return u - ((127 - 15) << 3);
+}
+__device__ __forceinline__ float pack_scale(uint32_t code) {
+  return __half2float(__ushort_as_half((unsigned short)(code << 7)));
+}
+
+// ---- kernels (k_packed.cu, k_packed_attn.cu) ----
+
+// Positions of a call in segments of one page each.  A run of consecutive positions
+// needs no table; a few come with the launch, more lie in device memory.
+constexpr int PACK_INLINE_POS = 512;
+struct PackedRows {
+  int n = 0, n_seg = 0;
+  int first = -1;                  // >= 0: positions first .. first + n - 1
+  const int32_t *pos_d = nullptr;  // device [n], then segment starts [n_seg + 1]
+  uint16_t seg[PACK_INLINE_POS + 1];
+  int32_t pos[PACK_INLINE_POS];
+};
+// k, v: [n][nl][G][dh] in the model dtype; len: the document's length after the write.
+void launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows, int len, int l0,
+                         int nl, const void *k, const void *val, cudaStream_t s);
+void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, int l0, int nl,
+                        void *k, void *val, cudaStream_t s);
+
+// A tile of the attention: up to 8 query vectors (row * heads per KV head + head) of
+// rows of one document, their pages dealt to parts.
+constexpr int PACK_VEC = 8;
+struct PackedTile {
+  int32_t vec0, nvec, doc, part0, n_parts, pad[3];
+};
+struct PackedAttnArgs {
+  const void *q;
+  void *out;
+  int ldq;                  // row stride of q in elements
+  int dtype, H, G, grp, dh, layer;
+  float scale;              // log2(e) / sqrt(dh)
+  const PackedView *docs;   // device
+  const int32_t *row_pos, *row_doc;  // device [rows]
+  // dense: parts {tile, first page, end page, part of the tile}
+  const PackedTile *tiles;
+  const int4 *parts;
+  int n_parts;
+  // sparse: blocks [rows][G][n_blocks]
+  const int32_t *blocks;
+  int n_rows, n_blocks, parts_per_row;
+  float *ws_o;      // [part][G][PACK_VEC][dh]
+  float2 *ws_ml;    // [part][G][PACK_VEC]
+  int *counters;    // [tile][G], zero between calls
+  int *dev_flag;
+};
+int packed_attn_ctas_per_sm(int dtype);  // CTAs of packed_attn_warps() warps that an SM holds
+int packed_attn_warps();
+int packed_attn_max_blocks_per_part();
+size_t packed_attn_ws_floats(int n_parts, int G, int dh);
+const char *launch_packed_attention(const PackedAttnArgs &a, cudaStream_t s);
+// Blocks of each (row, KV head): blocks [rows][G][n_blocks].
+const char *launch_packed_select(const PackedAttnArgs &a, int max_pages, int32_t *blocks,
+                                 cudaStream_t s);
+
+// ---- of api.cu, for the packed entry points ----
+// words of 32 bits to the device, ahead of what is queued next on the model's stream
+kvr_status upload_words(kvr_model *m, void *dst, const void *src, size_t words);
+kvr_status grow_device(kvr_model *m, void *&buf, size_t &have, size_t need, const char *what);
+kvr_status synchronize(kvr_model *m);
+kvr_status flush_uploads(kvr_model *m);
+
+}  // namespace kvr
+
+// A document's packed cache.
+struct kvr_packed {
+  kvr_model *model = nullptr;
+  int n = 0, cap = 0, pages = 0;
+  uint8_t *blocks = nullptr;
+  int8_t *bounds = nullptr;
+  float *unit = nullptr;
+  bool poisoned = false;
+  kvr::PackedView view() const {
+    return kvr::PackedView{blocks, bounds, unit, pages, model->dims.G, model->dims.dh};
+  }
+};
+
+// Query rows over packed documents: the tables of a pass, used by every layer of it.
+struct kvr_rows {
+  kvr_model *model = nullptr;
+  std::vector<kvr_packed *> docs;  // null: freed since
+  std::vector<int32_t> doc_rows, pos;
+  int n_parts = 0, n_tiles = 0, max_pages = 0;
+  void *mem = nullptr;  // device tables
+  size_t mem_bytes = 0;
+  kvr::PackedView *docs_d = nullptr;
+  kvr::PackedTile *tiles_d = nullptr;
+  int4 *parts_d = nullptr;
+  int32_t *pos_d = nullptr, *doc_d = nullptr;
+};

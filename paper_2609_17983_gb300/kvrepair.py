@@ -34,6 +34,9 @@ POLICIES = {"editlocal": 0, "structural": 1, "attention": 2, "cacheblend": 3, "r
             "editlocal_boundary": 5}
 
 
+BLOCK = 64  # positions of a packed cache's block (KVR_BLOCK)
+
+
 class KvrError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{ERRORS.get(code, code)}: {msg}")
@@ -103,6 +106,18 @@ _sigs = {
     "kvr_transplant": ([_P, _P, _P, _I32], _I32),
     "kvr_answer_logprob": ([_P, _P, _P, _I32, _P, _I32, _P], _I32),
     "kvr_margin": ([_P, _P, _P, _I32, _P, _I32, _P, _I32, _P], _I32),
+    "kvr_packed_create": ([_P, _I32, ctypes.POINTER(_P)], _I32),
+    "kvr_packed_free": ([_P], None),
+    "kvr_packed_len": ([_P], _I32),
+    "kvr_packed_write": ([_P, _P, _I32, _I32, _I32, _P, _P], _I32),
+    "kvr_packed_read": ([_P, _P, _I32, _I32, _I32, _P, _P], _I32),
+    "kvr_packed_bounds": ([_P, _I32, _P, _P, _P], _I32),
+    "kvr_rows_create": ([_P, _P, _P, _I32, _P, ctypes.POINTER(_P)], _I32),
+    "kvr_rows_move": ([_P, _P], _I32),
+    "kvr_rows_free": ([_P], None),
+    "kvr_packed_attention": ([_P, _I32, _P, _I32, _P], _I32),
+    "kvr_packed_select": ([_P, _I32, _P, _I32, _I32, _P], _I32),
+    "kvr_packed_attention_blocks": ([_P, _I32, _P, _I32, _P, _I32, _P], _I32),
 }
 for _name, (_args, _res) in _sigs.items():
     _f = getattr(_lib, _name)
@@ -282,6 +297,80 @@ def kvr_margin(model, cache, prompt, a_new, a_old) -> float:
     return out.value
 
 
+def kvr_packed_create(model, capacity: int) -> ctypes.c_void_p:
+    out = ctypes.c_void_p()
+    _check(_lib.kvr_packed_create(model, capacity, ctypes.byref(out)))
+    return out
+
+
+def kvr_packed_free(packed):
+    _lib.kvr_packed_free(packed)
+
+
+def kvr_packed_len(packed) -> int:
+    return int(_lib.kvr_packed_len(packed))
+
+
+def kvr_packed_write(packed, positions, layer_begin: int, layer_end: int, k_dev_ptr: int,
+                     v_dev_ptr: int):
+    ps = _i32(positions)
+    _check(_lib.kvr_packed_write(packed, _ptr(ps), ps.size, layer_begin, layer_end, k_dev_ptr,
+                                 v_dev_ptr))
+
+
+def kvr_packed_read(packed, positions, layer_begin: int, layer_end: int, k_dev_ptr: int,
+                    v_dev_ptr: int):
+    ps = _i32(positions)
+    _check(_lib.kvr_packed_read(packed, _ptr(ps), ps.size, layer_begin, layer_end, k_dev_ptr,
+                                v_dev_ptr))
+
+
+def kvr_packed_bounds(packed, layer: int, n_kv_heads: int, head_dim: int):
+    nb = -(-kvr_packed_len(packed) // BLOCK)
+    hi = np.zeros((n_kv_heads, nb, head_dim), np.int8)
+    lo = np.zeros_like(hi)
+    unit = np.zeros((n_kv_heads, nb), np.float32)
+    _check(_lib.kvr_packed_bounds(packed, layer, hi.ctypes.data, lo.ctypes.data,
+                                  unit.ctypes.data))
+    return hi, lo, unit
+
+
+def kvr_rows_create(model, docs) -> ctypes.c_void_p:
+    """docs: list of (packed handle, positions of its rows)."""
+    handles = (ctypes.c_void_p * max(len(docs), 1))(*[d for d, _ in docs])
+    pos = [_i32(p) for _, p in docs]
+    counts = _i32([p.size for p in pos])
+    allpos = _i32(np.concatenate(pos) if pos else np.zeros(0, np.int32))
+    out = ctypes.c_void_p()
+    _check(_lib.kvr_rows_create(model, handles, counts.ctypes.data, len(docs),
+                                allpos.ctypes.data, ctypes.byref(out)))
+    return out
+
+
+def kvr_rows_move(rows, positions):
+    ps = _i32(positions)
+    _check(_lib.kvr_rows_move(rows, ps.ctypes.data))
+
+
+def kvr_rows_free(rows):
+    _lib.kvr_rows_free(rows)
+
+
+def kvr_packed_attention(rows, layer: int, q_dev_ptr: int, ldq: int, out_dev_ptr: int):
+    _check(_lib.kvr_packed_attention(rows, layer, q_dev_ptr, ldq, out_dev_ptr))
+
+
+def kvr_packed_select(rows, layer: int, q_dev_ptr: int, ldq: int, n_blocks: int,
+                      blocks_dev_ptr: int):
+    _check(_lib.kvr_packed_select(rows, layer, q_dev_ptr, ldq, n_blocks, blocks_dev_ptr))
+
+
+def kvr_packed_attention_blocks(rows, layer: int, q_dev_ptr: int, ldq: int, blocks_dev_ptr: int,
+                                n_blocks: int, out_dev_ptr: int):
+    _check(_lib.kvr_packed_attention_blocks(rows, layer, q_dev_ptr, ldq, blocks_dev_ptr, n_blocks,
+                                            out_dev_ptr))
+
+
 def kvr_cache_len(cache) -> int:
     return int(_lib.kvr_cache_len(cache))
 
@@ -434,7 +523,7 @@ class Model:
     def __init__(self, cfg: dict, weights: dict | None = None, seed: int = 0,
                  max_context: int = 8192, max_rows: int = 4096):
         self.cfg = dict(cfg)
-        self._caches = weakref.WeakSet()
+        self._caches = weakref.WeakSet()  # caches, packed caches and rows over them
         self.h = kvr_model_create(cfg, weights, seed, max_context, max_rows)
         _live_models.add(self)
 
@@ -465,6 +554,14 @@ class Model:
         """A cache holding the given K/V rows ([n][L][G][dh], cache dtype)."""
         dt = np.uint16 if self.cfg["dtype"] == "bf16" else np.float32
         return Cache(self, kvr_cache_load(self.h, tokens, k, v, dt))
+
+    def packed(self, capacity: int) -> "Packed":
+        """An empty packed cache (4 bits an entry) for up to `capacity` positions."""
+        return Packed(self, kvr_packed_create(self.h, capacity))
+
+    def rows(self, docs) -> "Rows":
+        """Query rows over packed documents; docs: list of (Packed, positions)."""
+        return Rows(self, docs)
 
     def select(self, cache: "Cache", policy: str, K: int, edit_start: int, new_tokens,
                seed: int = 0) -> np.ndarray:
@@ -555,3 +652,123 @@ class Cache:
         dt = np.uint16 if c["dtype"] == "bf16" else np.float32
         return kvr_cache_read_raw(self.h, positions, layer_begin, le, c["n_kv_heads"],
                                   c["head_dim"], dt, k_out, v_out)
+
+
+def _device(t, name: str, dtype: str, count: int) -> int:
+    """Address of a contiguous CUDA tensor of `count` entries."""
+    if not t.is_cuda or str(t.dtype) != dtype or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of {count} entries, "
+                         f"not {t.dtype}{list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+class Packed:
+    """A document's K/V in 4 bits (kvr_packed_*); rows are torch CUDA tensors in the model's
+    type, [positions][layers][n_kv_heads][head_dim]."""
+
+    def __init__(self, model: Model, handle):
+        self.model = model
+        self.h = handle
+        c = model.cfg
+        self._row = c["n_kv_heads"] * c["head_dim"]
+        self._dtype = "torch.bfloat16" if c["dtype"] == "bf16" else "torch.float32"
+        model._caches.add(self)
+
+    def close(self):
+        if getattr(self, "h", None):
+            if getattr(self.model, "h", None):
+                kvr_packed_free(self.h)
+            self.h = None
+
+    def __del__(self):
+        self.close()
+
+    @property
+    def n(self) -> int:
+        return kvr_packed_len(self.h)
+
+    def _rows(self, positions, layer_begin, layer_end, k, v):
+        ps = _i32(positions)
+        le = self.model.cfg["n_layers"] if layer_end is None else layer_end
+        count = ps.size * max(le - layer_begin, 0) * self._row
+        return (ps, layer_begin, le, _device(k, "k", self._dtype, count),
+                _device(v, "v", self._dtype, count))
+
+    def write(self, positions, k, v, layer_begin: int = 0, layer_end: int | None = None):
+        """Quantise k and v into the cache at `positions` (kvr_packed_write)."""
+        kvr_packed_write(self.h, *self._rows(positions, layer_begin, layer_end, k, v))
+
+    def read(self, positions, k_out, v_out, layer_begin: int = 0, layer_end: int | None = None):
+        """The stored rows into k_out and v_out (kvr_packed_read)."""
+        kvr_packed_read(self.h, *self._rows(positions, layer_begin, layer_end, k_out, v_out))
+
+    def bounds(self, layer: int = 0):
+        """hi, lo [n_kv_heads][blocks][head_dim] (int8) and unit [n_kv_heads][blocks]."""
+        c = self.model.cfg
+        return kvr_packed_bounds(self.h, layer, c["n_kv_heads"], c["head_dim"])
+
+
+class Rows:
+    """Query rows over packed documents (kvr_rows_*); q and out are torch CUDA tensors of
+    [rows][n_heads][head_dim] entries in the model's type."""
+
+    def __init__(self, model: Model, docs):
+        docs = [(d, _i32(p)) for d, p in docs]
+        self.model = model
+        self.h = None
+        self.docs = [d for d, _ in docs]  # kept alive
+        self.n = sum(p.size for _, p in docs)
+        c = model.cfg
+        self._row = c["n_heads"] * c["head_dim"]
+        self._heads = (c["n_heads"], c["head_dim"])
+        self._lists = self.n * c["n_kv_heads"]
+        self._dtype = "torch.bfloat16" if c["dtype"] == "bf16" else "torch.float32"
+        self.h = kvr_rows_create(model.h, [(d.h, p) for d, p in docs])
+        model._caches.add(self)
+
+    def close(self):
+        if getattr(self, "h", None):
+            if getattr(self.model, "h", None):
+                kvr_rows_free(self.h)
+            self.h = None
+
+    def __del__(self):
+        self.close()
+
+    def move(self, positions):
+        """New positions of the same rows (kvr_rows_move)."""
+        ps = _i32(positions)
+        if ps.size != self.n:
+            raise ValueError(f"{self.n} positions wanted, not {ps.size}")
+        kvr_rows_move(self.h, ps)
+
+    def _q(self, q):
+        """Address and row stride of q: contiguous, or rows [rows, n_heads, head_dim] apart."""
+        if q.is_contiguous() or q.dim() != 3:
+            return _device(q, "q", self._dtype, self.n * self._row), self._row
+        H, dh = self._heads
+        if (not q.is_cuda or str(q.dtype) != self._dtype or tuple(q.shape) != (self.n, H, dh) or
+                q.stride(2) != 1 or q.stride(1) != dh):
+            raise ValueError(f"q must be {self._dtype} [{self.n}, {H}, {dh}], heads contiguous")
+        return q.data_ptr(), q.stride(0)
+
+    def attention(self, layer: int, q, out, blocks=None):
+        """Attention over all positions up to a row's own, or over those of `blocks` alone
+        (int32 [rows][n_kv_heads][n_blocks], kvr_packed_attention_blocks)."""
+        qp, ldq = self._q(q)
+        op = _device(out, "out", self._dtype, self.n * self._row)
+        if blocks is None:
+            kvr_packed_attention(self.h, layer, qp, ldq, op)
+            return
+        nb = blocks.shape[-1]
+        kvr_packed_attention_blocks(self.h, layer, qp, ldq,
+                                    _device(blocks, "blocks", "torch.int32", self._lists * nb), nb,
+                                    op)
+
+    def select(self, layer: int, q, blocks_out):
+        """The blocks that each row attends to (kvr_packed_select) into blocks_out, int32
+        [rows][n_kv_heads][n_blocks]."""
+        qp, ldq = self._q(q)
+        nb = blocks_out.shape[-1]
+        kvr_packed_select(self.h, layer, qp, ldq, nb,
+                          _device(blocks_out, "blocks_out", "torch.int32", self._lists * nb))
