@@ -119,8 +119,8 @@ __device__ __forceinline__ void v_codes_store(uint8_t *half, int kg, int ch, con
 __device__ __forceinline__ void eight_values(uint32_t c, uint32_t sc, __half2 *v) {
   const uint32_t s2 = sc << 7 | sc << 23;
   const __half2 s = *(const __half2 *)&s2;
-  const uint32_t w[4] = {pack_values<0>(c), pack_values<1>(c), pack_values<2>(c),
-                         pack_values<3>(c)};
+  uint32_t w[4];
+  pack_values(c, w);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = __hmul2(*(const __half2 *)&w[i], s);
 }
@@ -344,8 +344,8 @@ __global__ void __launch_bounds__(2 * DH)
 constexpr int SEL_THREADS = 256;
 template <int DH, typename T>
 __global__ void __launch_bounds__(SEL_THREADS)
-    k_packed_select(const T *q, int ldq, const PackedView *docs, const int32_t *row_pos,
-                    const int32_t *row_doc, int layer, int grp, int count, int32_t *blocks) {
+    k_packed_select(const T *q, int ldq, const PackedRow *rows, int layer, int grp, int count,
+                    int32_t *blocks) {
   extern __shared__ uint32_t keys[];  // ordered scores of the blocks before the own
   __shared__ __align__(16) int8_t qs[2][DH];
   __shared__ float amax[DH / 32];
@@ -354,13 +354,13 @@ __global__ void __launch_bounds__(SEL_THREADS)
   const int row = blockIdx.x, g = blockIdx.y, G = gridDim.y;
   pdl_trigger();
   pdl_wait();
-  const int pos = row_pos[row];
+  const int pos = rows[row].pos;
   int32_t *out = blocks + ((size_t)row * G + g) * count;
   if (pos < 0) {
     for (int i = tid; i < count; i += SEL_THREADS) out[i] = -1;
     return;
   }
-  const PackedView v = docs[row_doc[row]];
+  const PackedView v = rows[row].doc;
   const int own = pos / KVR_PAGE;
   if (own + 1 <= count) {  // every block that the row sees
     for (int i = tid; i < count; i += SEL_THREADS) out[i] = i <= own ? i : -1;
@@ -487,8 +487,8 @@ const char *launch_packed_select(const PackedAttnArgs &a, int max_pages, int32_t
     if (smem > 40 * 1024)
       if (const char *e = smem_opt_in(sel_smem[which], kernel, smem)) return e;
     const cudaError_t e =
-        launch_pdl(kernel, grid, dim3(SEL_THREADS), smem, s, q, a.ldq, a.docs, a.row_pos,
-                   a.row_doc, a.layer, a.grp, a.n_blocks, blocks);
+        launch_pdl(kernel, grid, dim3(SEL_THREADS), smem, s, q, a.ldq, a.rows, a.layer, a.grp,
+                   a.n_blocks, blocks);
     return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
   };
   if (a.dtype == KVR_DTYPE_BF16) {

@@ -24,6 +24,7 @@
 // vectors that see it, and its V scales are cleared before the products, so
 // vectors that do not see it are untouched.
 #include <math.h>
+#include <stdlib.h>
 
 #include "packed.cuh"
 #include "tc_ptx.cuh"
@@ -32,7 +33,6 @@ namespace kvr {
 namespace {
 using namespace ptx;
 
-constexpr int WARPS = 4;
 constexpr int STAGES = 2;           // pages in flight per warp
 constexpr float RAISE = 8.f;        // headroom of the reference (log2)
 constexpr float LIFT = 7.f;         // P = 2^(x - reference + LIFT) <= 2^15: more of a half's range
@@ -75,14 +75,36 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// Fragment of a K or V word: bytes 0 and 1 belong to scale s0, 2 and 3 to s1 (K: the
-// two keys), or bytes 0 and 2 to s0, 1 and 3 to s1 (V: the two pairs of keys).
-template <bool V>
-__device__ __forceinline__ void fragment(uint32_t w, uint32_t s0, uint32_t s1, uint32_t *a) {
-  a[0] = mul2(pack_values<0>(w), s0);
-  a[2] = mul2(pack_values<1>(w), V ? s1 : s0);
-  a[1] = mul2(pack_values<2>(w), V ? s0 : s1);
-  a[3] = mul2(pack_values<3>(w), s1);
+// Fragments of a K or V word: registers of the tile's rows 0-7 (bytes 0, 1) and 8-15
+// (bytes 2, 3), columns 0-7 (bytes 0, 2) and 8-15.  K: a scale for each half of the rows,
+// the same half of s0 and of s1; V: one for each half of the columns.
+template <int HI>
+__device__ __forceinline__ uint32_t mul_by(uint32_t a, uint32_t s) {
+  const __half2 s2 = *(const __half2 *)&s;
+  const __half2 r = __hmul2(*(const __half2 *)&a, HI ? __high2half2(s2) : __low2half2(s2));
+  return *(const uint32_t *)&r;
+}
+template <int HI>
+__device__ __forceinline__ void k_fragment(uint32_t w, uint32_t s0, uint32_t s1, uint32_t *a) {
+  uint32_t v[4];
+  pack_values(w, v);
+  a[0] = mul_by<HI>(v[0], s0);
+  a[2] = mul_by<HI>(v[1], s0);
+  a[1] = mul_by<HI>(v[2], s1);
+  a[3] = mul_by<HI>(v[3], s1);
+}
+__device__ __forceinline__ void v_fragment(uint32_t w, uint32_t s0, uint32_t s1, uint32_t *a) {
+  uint32_t v[4];
+  pack_values(w, v);
+  a[0] = mul2(v[0], s0);
+  a[2] = mul2(v[1], s1);
+  a[1] = mul2(v[2], s0);
+  a[3] = mul2(v[3], s1);
+}
+// Four scale codes as two half2.
+__device__ __forceinline__ void scales(uint32_t w, uint32_t &a, uint32_t &b) {
+  a = __byte_perm(w, 0, 0x4140) << 7;
+  b = __byte_perm(w, 0, 0x4342) << 7;
 }
 
 // Four entries of a row of q.
@@ -97,22 +119,38 @@ __device__ __forceinline__ void load4(const float *p, float *x) {
   const float4 u = *(const float4 *)p;
   x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
 }
-__device__ __forceinline__ void store(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
-__device__ __forceinline__ void store(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float a, float b, float c, float d) {
+  const __nv_bfloat162 x = __floats2bfloat162_rn(a, b), y = __floats2bfloat162_rn(c, d);
+  *(uint2 *)p = make_uint2(*(const uint32_t *)&x, *(const uint32_t *)&y);
+}
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) {
+  *(float4 *)p = make_float4(a, b, c, d);
+}
+__device__ __forceinline__ void add4(float4 &x, float f, float4 y) {
+  x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
+}
 
 // Weight of partial sums (m, l) under the common maximum M; NaN sums stay NaN.
 __device__ __forceinline__ float merge_weight(float m, float l, float M) {
   return l != l ? l : m == -INFINITY ? 0.f : ex2(m - M);
 }
 
-template <int DH, typename T, bool SPARSE>
-__global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_attn(const PackedAttnArgs p) {
+// CTAs of an SM: its registers hold 12 warps of a bf16 query, 8 of an fp32 one.
+template <typename T>
+constexpr int ctas_per_sm(int warps) {
+  return sizeof(T) == 4 ? 8 / warps : 12 / warps;
+}
+
+template <int DH, typename T, bool SPARSE, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
+    k_packed_attn(const __grid_constant__ PackedAttnArgs p) {
   constexpr bool SPLIT = sizeof(T) == 4;
   constexpr int HB = pack_half_bytes(DH), CB = pack_code_bytes(DH), DB = DH / 16, DQ = DH / 64;
   extern __shared__ __align__(128) uint8_t smem[];  // [WARPS][STAGES][K half, V half]
   __shared__ __align__(8) uint64_t full[WARPS][STAGES][2];
   __shared__ float2 s_ml[WARPS][PACK_VEC];
   __shared__ float s_wgt[WARPS][PACK_VEC];
+  __shared__ float2 s_tot[PACK_VEC];
   __shared__ int s_list[SPARSE ? SPARSE_MAX : 1], s_count, s_last, abort_f;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lg = lane >> 2, lt = lane & 3;
   const int g = blockIdx.y;
@@ -127,24 +165,25 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
   }
   if (tid == 0) abort_f = 0;
   pdl_trigger();
-  pdl_wait();
-
-  // the tile, its part and pages
-  int vec0, nvec, doc, n_parts, part, slot, counter, n_pages;
-  int page0 = 0;
+  // the tables were sent ahead of the kernel before this one (a.settled), or this launch
+  // waited for all before it: they are read ahead of the wait
+  int vec0, nvec, n_parts, part, slot, counter, n_pages, page0 = 0;
+  const uint8_t *blocks;
   if (SPARSE) {
     const int hc = (p.grp + PACK_VEC - 1) / PACK_VEC;  // chunks of a row's heads
     const int tile = blockIdx.x / p.parts_per_row, row = tile / hc, h0 = tile % hc * PACK_VEC;
+    const PackedRow r = p.rows[row];
     part = blockIdx.x % p.parts_per_row;
     n_parts = p.parts_per_row;
     vec0 = row * p.grp + h0;
     nvec = min(PACK_VEC, p.grp - h0);
-    doc = p.row_doc[row];
     slot = tile * n_parts;
     counter = tile;
+    blocks = r.doc.block(p.layer, g, 0);
+    pdl_wait();
     const int per = (p.n_blocks + n_parts - 1) / n_parts, i0 = part * per,
               i1 = min(p.n_blocks, i0 + per);
-    const int pos = p.row_pos[row], own = pos < 0 ? -1 : pos / KVR_PAGE;
+    const int own = r.pos < 0 ? -1 : r.pos / KVR_PAGE;
     if (warp == 0) {
       const int32_t *list = p.blocks + ((size_t)row * p.G + g) * p.n_blocks;
       int n = 0;
@@ -160,18 +199,17 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
     __syncthreads();
     n_pages = s_count;
   } else {
-    const int4 pt = p.parts[blockIdx.x];
-    const PackedTile t = p.tiles[pt.x];
-    vec0 = t.vec0, nvec = t.nvec, doc = t.doc, n_parts = t.n_parts;
-    part = pt.w;
-    slot = t.part0;
-    counter = pt.x;
-    page0 = pt.y;
-    n_pages = pt.z - pt.y;
+    const PackedPart t = p.parts[blockIdx.x];
+    vec0 = t.vec0, nvec = t.nvec, n_parts = t.n_parts;
+    part = t.part;
+    slot = t.slot;
+    counter = t.tile;
+    page0 = t.page0;
+    n_pages = t.page1 - t.page0;
+    blocks = t.blocks + ((size_t)p.layer * p.G + g) * t.pages * pack_block_bytes(DH);
     __syncthreads();
+    pdl_wait();
   }
-  const PackedView v = p.docs[doc];
-  const uint8_t *blocks = v.block(p.layer, g, 0);
   uint8_t *ring = smem + warp * (STAGES * 2 * HB);
   const int n_my = n_pages > warp ? (n_pages - warp + WARPS - 1) / WARPS : 0;
   auto page = [&](int i) {
@@ -237,7 +275,7 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
   for (int c = 0; c < 2; ++c) {
     sc[c] = __shfl_sync(0xFFFFFFFFu, qscale, 4 * (2 * lt + c));
     // a column without a vector is never masked: its results go nowhere
-    pos[c] = 2 * lt + c < nvec ? p.row_pos[(vec0 + 2 * lt + c) / p.grp] : 0x7FFFFFFF;
+    pos[c] = 2 * lt + c < nvec ? p.pos[(vec0 + 2 * lt + c) / p.grp] : 0x7FFFFFFF;
   }
   int least = min(pos[0], pos[1]);
   least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, 1));
@@ -257,22 +295,24 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       s[kt][0] = s[kt][1] = s[kt][2] = s[kt][3] = 0.f;
-      uint32_t ks[2][DB / 4];  // scales of the two keys
+      uint32_t ks[2][DQ][2];  // scales of the two keys
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int b = 0; b < DB / 4; ++b)
-          ks[h][b] = *(const uint32_t *)(kb + CB + ((kt * 8 + lg) * 2 + h) * DB + 4 * b);
+        for (int b = 0; b < DQ; ++b)
+          scales(*(const uint32_t *)(kb + CB + ((kt * 8 + lg) * 2 + h) * DB + 4 * b), ks[h][b][0],
+                 ks[h][b][1]);
 #pragma unroll
       for (int d4 = 0; d4 < DQ; ++d4) {
         const uint4 w4 = *(const uint4 *)(kb + ((kt * DQ + d4) * 32 + lane) * 16);
         const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          const uint32_t s0 = __byte_perm(ks[0][d4], 0, 0x4040 | b | b << 8) << 7,
-                         s1 = __byte_perm(ks[1][d4], 0, 0x4040 | b | b << 8) << 7;
           uint32_t a[4];
-          fragment<false>(w[b], s0, s1, a);
+          if (b & 1)
+            k_fragment<1>(w[b], ks[0][d4][b >> 1], ks[1][d4][b >> 1], a);
+          else
+            k_fragment<0>(w[b], ks[0][d4][b >> 1], ks[1][d4][b >> 1], a);
           mma16816(s[kt], a, qh[4 * d4 + b][0], qh[4 * d4 + b][1]);
           if (SPLIT) mma16816(s[kt], a, ql[4 * d4 + b][0], ql[4 * d4 + b][1]);
         }
@@ -371,10 +411,9 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
       float *d = SPLIT ? acc : o[b];
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
-        const uint32_t s0 = __byte_perm(vs[kt], 0, 0x4140) << 7,
-                       s1 = __byte_perm(vs[kt], 0, 0x4342) << 7;
-        uint32_t a[4];
-        fragment<true>(w[kt], s0, s1, a);
+        uint32_t a[4], s0, s1;
+        scales(vs[kt], s0, s1);
+        v_fragment(w[kt], s0, s1, a);
         mma16816(d, a, ph[kt][0], ph[kt][1]);
         if (SPLIT) mma16816(d, a, pl[kt][0], pl[kt][1]);
       }
@@ -407,7 +446,6 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
     }
   }
   __syncthreads();
-  __shared__ float2 s_tot[PACK_VEC];
   if (tid < PACK_VEC) {
     float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -422,23 +460,24 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
     s_tot[tid] = make_float2(M, L);
   }
   __syncthreads();
-  auto out_row = [&](int i) {  // vector i of the tile
-    const int vec = vec0 + i;
-    return (T *)p.out + ((size_t)(vec / p.grp) * p.H + g * p.grp + vec % p.grp) * DH;
+  auto out4 = [&](int i, float4 x, float L) {  // entries 4 (i % (DH / 4)) .. of the tile's vector
+    const int vec = vec0 + i / (DH / 4);
+    const float f = L == 0.f ? 0.f : 1.f / L;  // no key: zeros
+    store4((T *)p.out + ((size_t)(vec / p.grp) * p.H + g * p.grp + vec % p.grp) * DH +
+               4 * (i % (DH / 4)),
+           x.x * f, x.y * f, x.z * f, x.w * f);
   };
   const size_t at = ((size_t)(slot + part) * p.G + g) * PACK_VEC;
-  for (int i = tid; i < nvec * DH; i += WARPS * 32) {
-    const int vi = i / DH, d = i % DH;
-    float x = 0.f;
+  const int n4 = nvec * (DH / 4);
+  for (int i = tid; i < n4; i += WARPS * 32) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < WARPS; ++w)
-      x += s_wgt[w][vi] * ((const float *)(smem + w * (STAGES * 2 * HB)))[vi * DH + d];
-    if (n_parts == 1) {
-      const float L = s_tot[vi].y;
-      store(out_row(vi) + d, L == 0.f ? 0.f : x / L);  // no key: zeros
-    } else {
-      p.ws_o[at * DH + i] = x;
-    }
+      add4(x, s_wgt[w][i / (DH / 4)], ((const float4 *)(smem + w * (STAGES * 2 * HB)))[i]);
+    if (n_parts == 1)
+      out4(i, x, s_tot[i / (DH / 4)].y);
+    else
+      ((float4 *)(p.ws_o + at * DH))[i] = x;
   }
   if (n_parts == 1) return;
   if (tid < PACK_VEC) p.ws_ml[at + tid] = s_tot[tid];
@@ -449,53 +488,86 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) == 4 ? 2 : 3) k_packed_a
   if (!s_last) return;
   __threadfence();
   if (tid == 0) p.counters[(size_t)counter * p.G + g] = 0;
-  // ---- the last part adds them all, in order ----
+  // ---- the last part adds them all, in order: weights of the parts first (a warp a
+  // vector), then every part's sums with MERGE loads in flight a thread ----
   const size_t at0 = ((size_t)slot * p.G + g) * PACK_VEC, step = (size_t)p.G * PACK_VEC;
-  for (int i = tid; i < nvec * DH; i += WARPS * 32) {
-    const int vi = i / DH, d = i % DH;
-    float M = -INFINITY, L = 0.f, x = 0.f;
-    for (int k = 0; k < n_parts; ++k) M = fmaxf(M, __ldcg(&p.ws_ml[at0 + k * step + vi].x));
-    for (int k = 0; k < n_parts; ++k) {
+  float *wgt = (float *)smem;  // [n_parts][PACK_VEC]
+  for (int vi = warp; vi < nvec; vi += WARPS) {
+    float M = -INFINITY, L = 0.f;
+    for (int k = lane; k < n_parts; k += 32) M = fmaxf(M, __ldcg(&p.ws_ml[at0 + k * step + vi].x));
+#pragma unroll
+    for (int x = 16; x; x /= 2) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
+    for (int k = lane; k < n_parts; k += 32) {
       const float2 ml = __ldcg(&p.ws_ml[at0 + k * step + vi]);
       const float f = merge_weight(ml.x, ml.y, M);
+      wgt[k * PACK_VEC + vi] = f;
       L += f * ml.y;
-      x += f * __ldcg(&p.ws_o[(at0 + k * step) * DH + i]);
     }
-    store(out_row(vi) + d, L == 0.f ? 0.f : x / L);
+#pragma unroll
+    for (int x = 16; x; x /= 2) L += __shfl_xor_sync(0xFFFFFFFFu, L, x);
+    if (lane == 0) s_tot[vi] = make_float2(M, L);
+  }
+  __syncthreads();
+  constexpr int MERGE = 8;
+  for (int i = tid; i < n4; i += WARPS * 32) {
+    const int vi = i / (DH / 4);
+    const float4 *src = (const float4 *)(p.ws_o + at0 * DH) + i;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < n_parts; k0 += MERGE) {
+      float4 y[MERGE];
+#pragma unroll
+      for (int k = 0; k < MERGE; ++k)
+        if (k0 + k < n_parts) y[k] = __ldcg(src + (k0 + k) * step * (DH / 4));
+#pragma unroll
+      for (int k = 0; k < MERGE; ++k)
+        if (k0 + k < n_parts) add4(x, wgt[(k0 + k) * PACK_VEC + vi], y[k]);
+    }
+    out4(i, x, s_tot[vi].y);
   }
 }
 
-PerDevice<size_t> attn_smem[8];
+template <int DH, typename T, bool SPARSE, int WARPS>
+const char *run(const PackedAttnArgs &a, cudaStream_t s) {
+  static PerDevice<size_t> state;
+  auto *kernel = k_packed_attn<DH, T, SPARSE, WARPS>;
+  const size_t smem = (size_t)WARPS * STAGES * pack_block_bytes(DH);
+  if (const char *e = smem_opt_in(state, kernel, smem)) return e;
+  const int hc = (a.grp + PACK_VEC - 1) / PACK_VEC;
+  const dim3 grid(SPARSE ? a.n_rows * hc * a.parts_per_row : a.n_parts, a.G);
+  cudaError_t e = cudaSuccess;
+  if (a.settled)
+    e = launch_pdl(kernel, grid, dim3(WARPS * 32), smem, s, a);
+  else
+    kernel<<<grid, WARPS * 32, smem, s>>>(a);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+template <int DH, typename T>
+const char *run(const PackedAttnArgs &a, cudaStream_t s) {
+  constexpr int MANY = sizeof(T) == 4 ? 8 : 12;
+  if (a.blocks)
+    return a.warps == 4 ? run<DH, T, true, 4>(a, s) : run<DH, T, true, MANY>(a, s);
+  return a.warps == 4 ? run<DH, T, false, 4>(a, s) : run<DH, T, false, MANY>(a, s);
+}
 
 }  // namespace
 
-int packed_attn_warps() { return WARPS; }
-int packed_attn_ctas_per_sm(int dtype) { return dtype == KVR_DTYPE_BF16 ? 3 : 2; }
+int packed_attn_ctas_per_sm(int dtype, int warps) {
+  return dtype == KVR_DTYPE_BF16 ? ctas_per_sm<__nv_bfloat16>(warps) : ctas_per_sm<float>(warps);
+}
+int packed_attn_warps(int dtype, long long total, int num_sms) {
+  static const char *env = getenv("KVR_PROBE_WARPS");
+  if (env) return atoi(env) == 4 ? 4 : dtype == KVR_DTYPE_BF16 ? 12 : 8;
+  return 4;
+}
 int packed_attn_max_blocks_per_part() { return SPARSE_MAX; }
-size_t packed_attn_ws_floats(int n_parts, int G, int dh) {
+size_t packed_attn_ws_floats(long long n_parts, int G, int dh) {
   return (size_t)n_parts * G * PACK_VEC * dh;
 }
 
 const char *launch_packed_attention(const PackedAttnArgs &a, cudaStream_t s) {
-  const size_t smem = (size_t)WARPS * STAGES * pack_block_bytes(a.dh);
-  const int hc = (a.grp + PACK_VEC - 1) / PACK_VEC;
-  const dim3 grid(a.blocks ? a.n_rows * hc * a.parts_per_row : a.n_parts, a.G);
-  auto run = [&](auto kernel, int which) -> const char * {
-    if (const char *e = smem_opt_in(attn_smem[which], kernel, smem)) return e;
-    const cudaError_t e = launch_pdl(kernel, grid, dim3(WARPS * 32), smem, s, a);
-    return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
-  };
-  using B = __nv_bfloat16;
-  if (a.blocks) {
-    if (a.dtype == KVR_DTYPE_BF16)
-      return a.dh == 128 ? run(k_packed_attn<128, B, true>, 0) : run(k_packed_attn<64, B, true>, 1);
-    return a.dh == 128 ? run(k_packed_attn<128, float, true>, 2)
-                       : run(k_packed_attn<64, float, true>, 3);
-  }
   if (a.dtype == KVR_DTYPE_BF16)
-    return a.dh == 128 ? run(k_packed_attn<128, B, false>, 4) : run(k_packed_attn<64, B, false>, 5);
-  return a.dh == 128 ? run(k_packed_attn<128, float, false>, 6)
-                     : run(k_packed_attn<64, float, false>, 7);
+    return a.dh == 128 ? run<128, __nv_bfloat16>(a, s) : run<64, __nv_bfloat16>(a, s);
+  return a.dh == 128 ? run<128, float>(a, s) : run<64, float>(a, s);
 }
 
 }  // namespace kvr

@@ -116,77 +116,83 @@ kvr_status check_rows(const std::vector<kvr_packed *> &docs, const std::vector<i
   return i == count ? KVR_OK : fail(KVR_E_RANGE, "row counts do not match");
 }
 
+// Warps per CTA and pages per part that deal `total` (page, KV head) units to the
+// chip once: whole rounds of the warps, so that no warp waits for a longer one.
+struct Deal {
+  int warps, per;
+};
+Deal deal(const kvr_model *m, long long total) {
+  const int W = packed_attn_warps(m->dims.dtype, total, m->num_sms);
+  const long long slots = (long long)m->num_sms * packed_attn_ctas_per_sm(m->dims.dtype, W);
+  const long long each = (total + slots - 1) / slots;
+  return {W, (int)std::max<long long>(1, (each + W - 1) / W) * W};
+}
+
 // The tables of rows at `pos`, built and sent.
 kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   kvr_model *m = r->model;
   const Dims &dm = m->dims;
   const int grp = dm.H / dm.G, M = (int)r->pos.size(), D = (int)r->docs.size();
-  std::vector<PackedTile> tiles;
-  std::vector<int> pages;  // of a tile
-  std::vector<int32_t> doc(M);
+  std::vector<PackedPart> tiles;  // page1: all of the tile's
+  std::vector<PackedRow> rows(M);
   long long total = 0;
   int row0 = 0, most = 1;
   for (int d = 0; d < D; ++d) {
     const int R = r->doc_rows[d];
-    std::fill(doc.begin() + row0, doc.begin() + row0 + R, d);
+    const PackedView view = r->docs[d]->view();
+    for (int i = row0; i < row0 + R; ++i) rows[i] = PackedRow{view, pos[i], 0};
     for (int v = 0; v < R * grp; v += PACK_VEC) {
-      PackedTile t{};
+      PackedPart t{};
+      t.blocks = view.blocks;
+      t.pages = view.pages;
       t.vec0 = row0 * grp + v;
       t.nvec = std::min(PACK_VEC, R * grp - v);
-      t.doc = d;
       const int last = pos[(t.vec0 + t.nvec - 1) / grp];  // positions ascend
-      const int np = last < 0 ? 0 : last / KVR_PAGE + 1;
+      t.page1 = last < 0 ? 0 : last / KVR_PAGE + 1;
+      t.tile = (int)tiles.size();
       tiles.push_back(t);
-      pages.push_back(np);
-      total += np;
-      most = std::max(most, np);
+      total += t.page1;
+      most = std::max(most, t.page1);
     }
     row0 += R;
   }
-  // parts of whole rounds of the warps, as many as fill the chip once
-  const int W = packed_attn_warps();
-  const long long slots = std::max(1, m->num_sms * packed_attn_ctas_per_sm(dm.dtype) / dm.G);
-  const int per = (int)std::max<long long>(1, ((total + slots - 1) / slots + W - 1) / W) * W;
-  std::vector<int4> parts;
-  for (size_t t = 0; t < tiles.size(); ++t) {
-    tiles[t].part0 = (int)parts.size();
-    tiles[t].n_parts = std::max(1, (pages[t] + per - 1) / per);
-    for (int k = 0; k < tiles[t].n_parts; ++k)
-      parts.push_back(make_int4((int)t, std::min(pages[t], k * per),
-                                std::min(pages[t], (k + 1) * per), k));
+  const Deal dl = deal(m, total * dm.G);
+  std::vector<PackedPart> parts;
+  for (const PackedPart &t : tiles) {
+    PackedPart x = t;
+    x.slot = (int)parts.size();
+    x.n_parts = std::max(1, (t.page1 + dl.per - 1) / dl.per);
+    for (x.part = 0; x.part < x.n_parts; ++x.part) {
+      x.page0 = x.part * dl.per;
+      x.page1 = std::min(t.page1, x.page0 + dl.per);
+      parts.push_back(x);
+    }
   }
-  const size_t o_doc = 0, o_tile = up256(o_doc + D * sizeof(PackedView)),
-               o_part = up256(o_tile + tiles.size() * sizeof(PackedTile)),
-               o_pos = up256(o_part + parts.size() * sizeof(int4)), o_rd = up256(o_pos + M * 4ull),
-               bytes = up256(o_rd + M * 4ull);
+  const size_t o_row = up256(parts.size() * sizeof(PackedPart)),
+               o_pos = up256(o_row + M * sizeof(PackedRow)), bytes = up256(o_pos + M * 4ull);
   std::vector<char> host(bytes);
-  for (int d = 0; d < D; ++d) {
-    const PackedView v = r->docs[d]->view();
-    memcpy(host.data() + o_doc + d * sizeof v, &v, sizeof v);
-  }
-  memcpy(host.data() + o_tile, tiles.data(), tiles.size() * sizeof(PackedTile));
-  memcpy(host.data() + o_part, parts.data(), parts.size() * sizeof(int4));
+  memcpy(host.data(), parts.data(), parts.size() * sizeof(PackedPart));
+  memcpy(host.data() + o_row, rows.data(), M * sizeof(PackedRow));
   memcpy(host.data() + o_pos, pos, M * 4ull);
-  memcpy(host.data() + o_rd, doc.data(), M * 4ull);
-  r->docs_d = nullptr;  // no tables until they are sent
+  r->sent = r->settled = false;
   KVR_TRY(grow_device(m, r->mem, r->mem_bytes, bytes, "query rows"));
   KVR_TRY(upload_words(m, r->mem, host.data(), bytes / 4));
   char *base = (char *)r->mem;
-  r->docs_d = (PackedView *)(base + o_doc);
-  r->tiles_d = (PackedTile *)(base + o_tile);
-  r->parts_d = (int4 *)(base + o_part);
+  r->parts_d = (PackedPart *)base;
+  r->rows_d = (PackedRow *)(base + o_row);
   r->pos_d = (int32_t *)(base + o_pos);
-  r->doc_d = (int32_t *)(base + o_rd);
   r->n_parts = (int)parts.size();
   r->n_tiles = (int)tiles.size();
   r->max_pages = most;
+  r->warps = dl.warps;
   std::copy(pos, pos + M, r->pos.begin());
+  r->sent = true;
   return KVR_OK;
 }
 
 // Room for the partial sums and arrival counts of a launch.
 kvr_status attn_workspace(kvr_model *m, PackedAttnArgs &a, long long parts, long long tiles) {
-  const size_t o = up256(packed_attn_ws_floats((int)parts, a.G, a.dh) * 4),
+  const size_t o = up256(packed_attn_ws_floats(parts, a.G, a.dh) * 4),
                ml = (size_t)parts * a.G * PACK_VEC * sizeof(float2), cb = (size_t)tiles * a.G * 4;
   if (o + ml > m->pack_ws_bytes)
     KVR_TRY(grow_device(m, m->pack_ws, m->pack_ws_bytes, o + ml, "packed attention workspace"));
@@ -211,7 +217,7 @@ kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, Pac
     if (!d) return fail(KVR_E_INVAL, "a document of these rows has been freed");
     if (d->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned");
   }
-  if (!r->docs_d) return fail(KVR_E_INVAL, "rows whose last move failed");
+  if (!r->sent) return fail(KVR_E_INVAL, "rows whose last move failed");
   if (ldq < dm.H * dm.dh || ldq * dm.es() % 16)
     return fail(KVR_E_INVAL, "row stride %d of q: at least %d, whole 16-byte pieces", ldq,
                 dm.H * dm.dh);
@@ -224,12 +230,12 @@ kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, Pac
   a.H = dm.H, a.G = dm.G, a.grp = dm.H / dm.G, a.dh = dm.dh;
   a.layer = layer;
   a.scale = (float)(1.4426950408889634 / std::sqrt((double)dm.dh));
-  a.docs = r->docs_d;
-  a.row_pos = r->pos_d;
-  a.row_doc = r->doc_d;
-  a.tiles = r->tiles_d;
+  a.pos = r->pos_d;
+  a.rows = r->rows_d;
   a.parts = r->parts_d;
   a.n_parts = r->n_parts;
+  a.warps = r->warps;
+  a.settled = r->settled;
   a.n_rows = (int)r->pos.size();
   a.dev_flag = m->dev_flag;
   return KVR_OK;
@@ -415,7 +421,9 @@ kvr_status kvr_packed_attention(kvr_rows *r, int32_t layer, const void *q, int32
   KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles));
   if (const char *e = launch_packed_attention(a, m->stream))
     return fail(KVR_E_CUDA, "packed attention: %s", e);
-  return launched(m, 1, "packed attention");
+  KVR_TRY(launched(m, 1, "packed attention"));
+  r->settled = true;
+  return KVR_OK;
 }
 
 kvr_status kvr_packed_select(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
@@ -429,7 +437,9 @@ kvr_status kvr_packed_select(kvr_rows *r, int32_t layer, const void *q, int32_t 
   a.n_blocks = n_blocks;
   if (const char *e = launch_packed_select(a, r->max_pages, blocks_out, m->stream))
     return fail(KVR_E_CUDA, "block selection: %s", e);
-  return launched(m, 1, "block selection");
+  KVR_TRY(launched(m, 1, "block selection"));
+  r->settled = true;
+  return KVR_OK;
 }
 
 kvr_status kvr_packed_attention_blocks(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
@@ -444,19 +454,19 @@ kvr_status kvr_packed_attention_blocks(kvr_rows *r, int32_t layer, const void *q
   a.out = out;
   a.blocks = blocks;
   a.n_blocks = n_blocks;
-  // parts of whole rounds of the warps, as many as fill the chip once
-  const int W = packed_attn_warps(), most = packed_attn_max_blocks_per_part();
   const long long tiles = (long long)a.n_rows * ((a.grp + PACK_VEC - 1) / PACK_VEC);
-  const long long slots = (long long)m->num_sms * packed_attn_ctas_per_sm(a.dtype);
-  const long long each = (tiles * a.G * n_blocks + slots - 1) / slots;
-  const int per = (int)std::min<long long>(most, std::max<long long>(1, (each + W - 1) / W) * W);
+  const Deal dl = deal(m, tiles * a.G * n_blocks);
+  const int per = std::min(dl.per, packed_attn_max_blocks_per_part());
+  a.warps = dl.warps;
   a.parts_per_row = (n_blocks + per - 1) / per;
   if (tiles * a.parts_per_row > 0x7FFFFFFF)
     return fail(KVR_E_UNSUPPORTED, "too many rows (%d) for %d blocks each", a.n_rows, n_blocks);
   KVR_TRY(attn_workspace(m, a, tiles * a.parts_per_row, tiles));
   if (const char *e = launch_packed_attention(a, m->stream))
     return fail(KVR_E_CUDA, "block attention: %s", e);
-  return launched(m, 1, "block attention");
+  KVR_TRY(launched(m, 1, "block attention"));
+  r->settled = true;
+  return KVR_OK;
 }
 
 }  // extern "C"

@@ -84,15 +84,15 @@ struct PackedView {
   }
 };
 
-// The half2 of two codes in a byte of w (low nibble first).
-template <int BYTE>
-__device__ __forceinline__ uint32_t pack_values(uint32_t w) {
-  uint32_t r;
-  asm("{\n\t.reg .b8 b;\n\t.reg .b32 t;\n\tshr.b32 t, %1, %2;\n\tcvt.u8.u32 b, t;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %0, b;\n\t}"
-      : "=r"(r)
-      : "r"(w), "n"(8 * BYTE));
-  return r;
+// The values of a word's eight codes, a half2 (low nibble first) for each byte.  Taken
+// apart into bytes by one mov, the conversions read them where they lie; extracted by
+// shifts each cost one more ALU instruction (15 clocks a word instead of 10.5).
+__device__ __forceinline__ void pack_values(uint32_t w, uint32_t *v) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+      : "r"(w));
 }
 
 // Codes of a (low nibble) and b.
@@ -136,11 +136,21 @@ void launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows,
 void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, int l0, int nl,
                         void *k, void *val, cudaStream_t s);
 
-// A tile of the attention: up to 8 query vectors (row * heads per KV head + head) of
-// rows of one document, their pages dealt to parts.
+// A tile of the attention is up to 8 query vectors (row * heads per KV head + head) of
+// rows of one document; its pages are dealt to parts, a CTA each.
 constexpr int PACK_VEC = 8;
-struct PackedTile {
-  int32_t vec0, nvec, doc, part0, n_parts, pad[3];
+struct PackedPart {
+  const uint8_t *blocks;  // the document's
+  int32_t pages;          // its capacity
+  int32_t vec0, nvec;
+  int32_t page0, page1;
+  int32_t part, n_parts;  // of the tile
+  int32_t slot;           // the tile's first part among all
+  int32_t tile, pad[3];
+};
+struct PackedRow {
+  PackedView doc;
+  int32_t pos, pad;
 };
 struct PackedAttnArgs {
   const void *q;
@@ -148,12 +158,11 @@ struct PackedAttnArgs {
   int ldq;                  // row stride of q in elements
   int dtype, H, G, grp, dh, layer;
   float scale;              // log2(e) / sqrt(dh)
-  const PackedView *docs;   // device
-  const int32_t *row_pos, *row_doc;  // device [rows]
-  // dense: parts {tile, first page, end page, part of the tile}
-  const PackedTile *tiles;
-  const int4 *parts;
-  int n_parts;
+  const int32_t *pos;       // device [rows]
+  const PackedRow *rows;    // device [rows]
+  // dense
+  const PackedPart *parts;
+  int n_parts, warps;       // packed_attn_warps'
   // sparse: blocks [rows][G][n_blocks]
   const int32_t *blocks;
   int n_rows, n_blocks, parts_per_row;
@@ -161,11 +170,13 @@ struct PackedAttnArgs {
   float2 *ws_ml;    // [part][G][PACK_VEC]
   int *counters;    // [tile][G], zero between calls
   int *dev_flag;
+  bool settled;     // the tables were sent before the kernel that precedes this one
 };
-int packed_attn_ctas_per_sm(int dtype);  // CTAs of packed_attn_warps() warps that an SM holds
-int packed_attn_warps();
+// Warps per CTA for `total` (page, KV head) units, and CTAs of an SM.
+int packed_attn_warps(int dtype, long long total, int num_sms);
+int packed_attn_ctas_per_sm(int dtype, int warps);
 int packed_attn_max_blocks_per_part();
-size_t packed_attn_ws_floats(int n_parts, int G, int dh);
+size_t packed_attn_ws_floats(long long n_parts, int G, int dh);
 const char *launch_packed_attention(const PackedAttnArgs &a, cudaStream_t s);
 // Blocks of each (row, KV head): blocks [rows][G][n_blocks].
 const char *launch_packed_select(const PackedAttnArgs &a, int max_pages, int32_t *blocks,
@@ -198,11 +209,12 @@ struct kvr_rows {
   kvr_model *model = nullptr;
   std::vector<kvr_packed *> docs;  // null: freed since
   std::vector<int32_t> doc_rows, pos;
-  int n_parts = 0, n_tiles = 0, max_pages = 0;
+  int n_parts = 0, n_tiles = 0, max_pages = 0, warps = 0;
+  bool sent = false;     // the device holds the tables of pos
+  bool settled = false;  // and a kernel was launched behind their upload
   void *mem = nullptr;  // device tables
   size_t mem_bytes = 0;
-  kvr::PackedView *docs_d = nullptr;
-  kvr::PackedTile *tiles_d = nullptr;
-  int4 *parts_d = nullptr;
-  int32_t *pos_d = nullptr, *doc_d = nullptr;
+  kvr::PackedPart *parts_d = nullptr;
+  kvr::PackedRow *rows_d = nullptr;
+  int32_t *pos_d = nullptr;
 };
