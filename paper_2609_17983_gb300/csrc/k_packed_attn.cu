@@ -17,14 +17,15 @@
 // q is scaled by a power of two per vector so that it is a half as exactly as it
 // was a bf16; an fp32 model's q and P go as two halves each (22 bits), with
 // a page's products added to O in fp32 registers.  All sums are in fp32.
-// The warps' (max, sum, O) meet in shared memory, the parts' in the workspace, where the
-// last part to arrive adds them in order.
+// The warps' (max, sum, O) meet in shared memory, those of a cluster's CTAs in one
+// another's shared memory, each adding a slice; of several clusters the last to arrive
+// adds them all, in order.
 //
 // A key whose row held a NaN or an infinity has NaN scales: its score is NaN for the
 // vectors that see it, and its V scales are cleared before the products, so
 // vectors that do not see it are untouched.
+#include <cooperative_groups.h>
 #include <math.h>
-#include <stdlib.h>
 
 #include "packed.cuh"
 #include "tc_ptx.cuh"
@@ -295,13 +296,18 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       s[kt][0] = s[kt][1] = s[kt][2] = s[kt][3] = 0.f;
-      uint32_t ks[2][DQ][2];  // scales of the two keys
+      uint32_t sw[2 * DQ], ks[2][DQ][2];  // scales of the two keys
+      if constexpr (DQ == 2) {
+        const uint4 u = *(const uint4 *)(kb + CB + (kt * 8 + lg) * 2 * DB);
+        sw[0] = u.x, sw[1] = u.y, sw[2] = u.z, sw[3] = u.w;
+      } else {
+        const uint2 u = *(const uint2 *)(kb + CB + (kt * 8 + lg) * 2 * DB);
+        sw[0] = u.x, sw[1] = u.y;
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int b = 0; b < DQ; ++b)
-          scales(*(const uint32_t *)(kb + CB + ((kt * 8 + lg) * 2 + h) * DB + 4 * b), ks[h][b][0],
-                 ks[h][b][1]);
+        for (int b = 0; b < DQ; ++b) scales(sw[h * DQ + b], ks[h][b][0], ks[h][b][1]);
 #pragma unroll
       for (int d4 = 0; d4 < DQ; ++d4) {
         const uint4 w4 = *(const uint4 *)(kb + ((kt * DQ + d4) * 32 + lane) * 16);
@@ -352,55 +358,66 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
     }
-    const bool masked = first + KVR_PAGE - 1 > least;
+    if (first + KVR_PAGE - 1 > least) {
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (first + 16 * kt + pack_key_of(lg) + (i & 2) > pos[i & 1]) s[kt][i] = -INFINITY;
+    }
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = i & 1, key = first + 16 * kt + pack_key_of(lg) + (i & 2);
-        s[kt][i] *= sc[c];
-        if (masked && key > pos[c]) s[kt][i] = -INFINITY;
-        top[c] = fmaxf(top[c], s[kt][i]);
-      }
+      for (int i = 0; i < 4; ++i) top[i & 1] = fmaxf(top[i & 1], s[kt][i]);
+    top[0] *= sc[0];  // scales are positive: the largest stays the largest
+    top[1] *= sc[1];
     if (__any_sync(0xFFFFFFFFu, top[0] > ref[0] + RAISE || top[1] > ref[1] + RAISE)) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
 #pragma unroll
         for (int x = 4; x < 32; x *= 2)
           top[c] = fmaxf(top[c], __shfl_xor_sync(0xFFFFFFFFu, top[c], x));
-        const float now = fmaxf(ref[c], top[c]);
-        const float f = ref[c] == -INFINITY ? 0.f : ex2(ref[c] - now);
-        if (now > ref[c]) {  // sums so far are zero where there was no reference
-          l[c] = ref[c] == -INFINITY ? l[c] : l[c] * f;
+        if (top[c] > ref[c]) {
+          if (ref[c] != -INFINITY) {  // before, all sums are zero (or NaN)
+            const float f = ex2(ref[c] - top[c]);
+            l[c] *= f;
 #pragma unroll
-          for (int b = 0; b < DB; ++b) {
-            if (ref[c] != -INFINITY) {
+            for (int b = 0; b < DB; ++b) {
               o[b][c] *= f;
               o[b][c + 2] *= f;
             }
           }
-          ref[c] = now;
+          ref[c] = top[c];
         }
       }
     }
     uint32_t ph[4][2], pl[SPLIT ? 4 : 1][2];  // fragments of P^T: 16 keys, lane's vector lg
     {
-      const float base[2] = {(ref[0] == -INFINITY ? 0.f : ref[0]) - LIFT,
-                             (ref[1] == -INFINITY ? 0.f : ref[1]) - LIFT};
+      const float base[2] = {LIFT - (ref[0] == -INFINITY ? 0.f : ref[0]),
+                             LIFT - (ref[1] == -INFINITY ? 0.f : ref[1])};
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float x = ex2(s[kt][2 * h] - base[0]), y = ex2(s[kt][2 * h + 1] - base[1]);
-          l[0] += x;
-          l[1] += y;
+          const float x = ex2(fmaf(s[kt][2 * h], sc[0], base[0])),
+                      y = ex2(fmaf(s[kt][2 * h + 1], sc[1], base[1]));
           const uint32_t u = half2_of(x, y);
           ph[kt][h] = transpose8x8(u);
           if (SPLIT) {
             const float2 f = __half22float2(*(const __half2 *)&u);
             pl[kt][h] = transpose8x8(half2_of(x - f.x, y - f.y));
+            l[0] += x;
+            l[1] += y;
           }
         }
+      if (!SPLIT) {  // the sums of the weights as they are used: a product with ones
+        float t[4] = {l[0], l[1], 0.f, 0.f};
+        const uint32_t ones[4] = {0x3C003C00u, 0, 0x3C003C00u, 0};  // rows 0-7
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) mma16816(t, ones, ph[kt][0], ph[kt][1]);
+        l[0] = t[0];
+        l[1] = t[1];
+      }
     }
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
@@ -437,7 +454,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
 #pragma unroll
-    for (int x = 4; x < 32; x *= 2) l[c] += __shfl_xor_sync(0xFFFFFFFFu, l[c], x);
+    for (int x = 4; x < 32 && SPLIT; x *= 2) l[c] += __shfl_xor_sync(0xFFFFFFFFu, l[c], x);
     if (lg == 0) s_ml[warp][2 * lt + c] = make_float2(ref[c], l[c]);
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
@@ -467,60 +484,110 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
                4 * (i % (DH / 4)),
            x.x * f, x.y * f, x.z * f, x.w * f);
   };
-  const size_t at = ((size_t)(slot + part) * p.G + g) * PACK_VEC;
-  const int n4 = nvec * (DH / 4);
-  for (int i = tid; i < n4; i += WARPS * 32) {
+  // ---- the cluster's sums: each CTA adds a slice of them, out of everyone's memory ----
+  const int cl = p.cluster, rank = part % cl, nc = n_parts / cl;
+  const int n4 = nvec * (DH / 4), per4 = (n4 + cl - 1) / cl;
+  const int i0 = min(n4, rank * per4), i1 = min(n4, i0 + per4);
+  const size_t slot0 = ((size_t)(slot / cl) * p.G + g), at = slot0 + (size_t)(part / cl) * p.G;
+  auto finish = [&](int i, float4 x, float M, float L) {
+    if (nc == 1) {
+      out4(i, x, L);
+      return;
+    }
+    ((float4 *)p.ws_o)[at * PACK_VEC * (DH / 4) + i] = x;
+    if (i == i0 || i % (DH / 4) == 0)
+      p.ws_ml[(at * PACK_CLUSTER + rank) * PACK_VEC + i / (DH / 4)] = make_float2(M, L);
+  };
+  auto warps_sum = [&](int i) {
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < WARPS; ++w)
       add4(x, s_wgt[w][i / (DH / 4)], ((const float4 *)(smem + w * (STAGES * 2 * HB)))[i]);
-    if (n_parts == 1)
-      out4(i, x, s_tot[i / (DH / 4)].y);
-    else
-      ((float4 *)(p.ws_o + at * DH))[i] = x;
+    return x;
+  };
+  if (cl == 1) {
+    for (int i = tid; i < n4; i += WARPS * 32)
+      finish(i, warps_sum(i), s_tot[i / (DH / 4)].x, s_tot[i / (DH / 4)].y);
+  } else {
+    namespace cg = cooperative_groups;
+    const cg::cluster_group cluster = cg::this_cluster();
+    float4 *sum = (float4 *)smem + PACK_VEC * (DH / 4);  // behind the first warp's sums
+    for (int i = tid; i < n4; i += WARPS * 32) sum[i] = warps_sum(i);
+    cluster.sync();
+    for (int i = i0 + tid; i < i1; i += WARPS * 32) {
+      const int vi = i / (DH / 4);
+      float2 ml[PACK_CLUSTER];
+      float4 y[PACK_CLUSTER];
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int k = 0; k < PACK_CLUSTER; ++k)
+        if (k < cl) {
+          ml[k] = *cluster.map_shared_rank(&s_tot[vi], k);
+          y[k] = *cluster.map_shared_rank(sum + i, k);
+          M = fmaxf(M, ml[k].x);
+        }
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < PACK_CLUSTER; ++k)
+        if (k < cl) {
+          const float f = merge_weight(ml[k].x, ml[k].y, M);
+          L += f * ml[k].y;
+          add4(x, f, y[k]);
+        }
+      finish(i, x, M, L);
+    }
+    // nobody leaves, or writes to its sums, while another reads them
+    cluster.sync();
   }
-  if (n_parts == 1) return;
-  if (tid < PACK_VEC) p.ws_ml[at + tid] = s_tot[tid];
+  if (nc == 1) return;
   __threadfence();
   __syncthreads();
-  if (tid == 0) s_last = atomicAdd(p.counters + (size_t)counter * p.G + g, 1) == n_parts - 1;
+  int *arrived = p.counters + ((size_t)counter * p.G + g) * PACK_CLUSTER + rank;
+  if (tid == 0) s_last = atomicAdd(arrived, 1) == nc - 1;
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  if (tid == 0) p.counters[(size_t)counter * p.G + g] = 0;
-  // ---- the last part adds them all, in order: weights of the parts first (a warp a
-  // vector), then every part's sums with MERGE loads in flight a thread ----
-  const size_t at0 = ((size_t)slot * p.G + g) * PACK_VEC, step = (size_t)p.G * PACK_VEC;
-  float *wgt = (float *)smem;  // [n_parts][PACK_VEC]
-  for (int vi = warp; vi < nvec; vi += WARPS) {
-    float M = -INFINITY, L = 0.f;
-    for (int k = lane; k < n_parts; k += 32) M = fmaxf(M, __ldcg(&p.ws_ml[at0 + k * step + vi].x));
+  if (tid == 0) *arrived = 0;
+  // ---- the last cluster's CTAs add the slices of all, in order: MERGE clusters' sums in
+  // flight a thread, the first of them while the weights are found (a warp a vector) ----
+  constexpr int MERGE = 20;
+  float *wgt = (float *)smem;  // [nc][PACK_VEC]
+  const size_t step = p.G;
+  const float4 *src = (const float4 *)p.ws_o + slot0 * PACK_VEC * (DH / 4);
+  float4 y[MERGE];
+  auto fetch_sums = [&](int i, int k0) {
 #pragma unroll
-    for (int x = 16; x; x /= 2) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
-    for (int k = lane; k < n_parts; k += 32) {
-      const float2 ml = __ldcg(&p.ws_ml[at0 + k * step + vi]);
-      const float f = merge_weight(ml.x, ml.y, M);
-      wgt[k * PACK_VEC + vi] = f;
-      L += f * ml.y;
+    for (int k = 0; k < MERGE; ++k)
+      if (k0 + k < nc) y[k] = __ldcg(src + i + (k0 + k) * step * PACK_VEC * (DH / 4));
+  };
+  if (i0 + tid < i1) fetch_sums(i0 + tid, 0);
+  if (i0 < i1)
+    for (int vi = i0 / (DH / 4) + warp; vi <= (i1 - 1) / (DH / 4); vi += WARPS) {
+      const float2 *part_ml = p.ws_ml + (slot0 * PACK_CLUSTER + rank) * PACK_VEC + vi;
+      float M = -INFINITY, L = 0.f;
+      for (int k = lane; k < nc; k += 32)
+        M = fmaxf(M, __ldcg(&part_ml[k * step * PACK_CLUSTER * PACK_VEC].x));
+#pragma unroll
+      for (int x = 16; x; x /= 2) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
+      for (int k = lane; k < nc; k += 32) {
+        const float2 ml = __ldcg(&part_ml[k * step * PACK_CLUSTER * PACK_VEC]);
+        const float f = merge_weight(ml.x, ml.y, M);
+        wgt[k * PACK_VEC + vi] = f;
+        L += f * ml.y;
+      }
+#pragma unroll
+      for (int x = 16; x; x /= 2) L += __shfl_xor_sync(0xFFFFFFFFu, L, x);
+      if (lane == 0) s_tot[vi] = make_float2(M, L);
     }
-#pragma unroll
-    for (int x = 16; x; x /= 2) L += __shfl_xor_sync(0xFFFFFFFFu, L, x);
-    if (lane == 0) s_tot[vi] = make_float2(M, L);
-  }
   __syncthreads();
-  constexpr int MERGE = 8;
-  for (int i = tid; i < n4; i += WARPS * 32) {
+  for (int i = i0 + tid; i < i1; i += WARPS * 32) {
     const int vi = i / (DH / 4);
-    const float4 *src = (const float4 *)(p.ws_o + at0 * DH) + i;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = 0; k0 < n_parts; k0 += MERGE) {
-      float4 y[MERGE];
+    for (int k0 = 0; k0 < nc; k0 += MERGE) {
+      if (k0 || i != i0 + tid) fetch_sums(i, k0);
 #pragma unroll
       for (int k = 0; k < MERGE; ++k)
-        if (k0 + k < n_parts) y[k] = __ldcg(src + (k0 + k) * step * (DH / 4));
-#pragma unroll
-      for (int k = 0; k < MERGE; ++k)
-        if (k0 + k < n_parts) add4(x, wgt[(k0 + k) * PACK_VEC + vi], y[k]);
+        if (k0 + k < nc) add4(x, wgt[(k0 + k) * PACK_VEC + vi], y[k]);
     }
     out4(i, x, s_tot[vi].y);
   }
@@ -534,11 +601,20 @@ const char *run(const PackedAttnArgs &a, cudaStream_t s) {
   if (const char *e = smem_opt_in(state, kernel, smem)) return e;
   const int hc = (a.grp + PACK_VEC - 1) / PACK_VEC;
   const dim3 grid(SPARSE ? a.n_rows * hc * a.parts_per_row : a.n_parts, a.G);
-  cudaError_t e = cudaSuccess;
-  if (a.settled)
-    e = launch_pdl(kernel, grid, dim3(WARPS * 32), smem, s, a);
-  else
-    kernel<<<grid, WARPS * 32, smem, s>>>(a);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(WARPS * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = a.cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = g_pdl && a.settled ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 template <int DH, typename T>
@@ -554,15 +630,7 @@ const char *run(const PackedAttnArgs &a, cudaStream_t s) {
 int packed_attn_ctas_per_sm(int dtype, int warps) {
   return dtype == KVR_DTYPE_BF16 ? ctas_per_sm<__nv_bfloat16>(warps) : ctas_per_sm<float>(warps);
 }
-int packed_attn_warps(int dtype, long long total, int num_sms) {
-  static const char *env = getenv("KVR_PROBE_WARPS");
-  if (env) return atoi(env) == 4 ? 4 : dtype == KVR_DTYPE_BF16 ? 12 : 8;
-  return 4;
-}
 int packed_attn_max_blocks_per_part() { return SPARSE_MAX; }
-size_t packed_attn_ws_floats(long long n_parts, int G, int dh) {
-  return (size_t)n_parts * G * PACK_VEC * dh;
-}
 
 const char *launch_packed_attention(const PackedAttnArgs &a, cudaStream_t s) {
   if (a.dtype == KVR_DTYPE_BF16)

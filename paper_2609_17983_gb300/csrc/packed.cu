@@ -116,16 +116,52 @@ kvr_status check_rows(const std::vector<kvr_packed *> &docs, const std::vector<i
   return i == count ? KVR_OK : fail(KVR_E_RANGE, "row counts do not match");
 }
 
-// Warps per CTA and pages per part that deal `total` (page, KV head) units to the
-// chip once: whole rounds of the warps, so that no warp waits for a longer one.
+// How tiles of `pages` pages each (times G KV heads) are dealt to the chip: warps of a
+// CTA, pages of a part, parts of a cluster.
 struct Deal {
-  int warps, per;
+  int warps, per, cluster;
+  int parts(int np) const {
+    const int n = std::max(1, (np + per - 1) / per);
+    return (n + cluster - 1) / cluster * cluster;
+  }
 };
-Deal deal(const kvr_model *m, long long total) {
-  const int W = packed_attn_warps(m->dims.dtype, total, m->num_sms);
-  const long long slots = (long long)m->num_sms * packed_attn_ctas_per_sm(m->dims.dtype, W);
-  const long long each = (total + slots - 1) / slots;
-  return {W, (int)std::max<long long>(1, (each + W - 1) / W) * W};
+
+// The deal whose launch is modelled to end first, in units of 10 ns.  A wave of CTAs costs
+// 5.2 us beside its rounds (a page for each of a CTA's warps), a round 1.35 and 0.1 per
+// warp that shares the SM; a cluster's sums 0.9, a merge through memory 3.1 and 0.04 per
+// cluster; clusters of 4 and 8 leave 1/20 and 1/4 of the SMs without a place.  Fitted to
+// 6900 launches of 1 to 64 rows over 64 to 131072 positions: the deal taken is 1.4% slower
+// than the fastest on average, 15% at most.  One token over 5000 positions, 4 KV heads: 8
+// CTAs of 12 warps as a cluster 7.4 us (merged through memory 9.2, with 4 warps 8.6); over
+// 131072, 8 KV heads: 19 CTAs of 12 warps a head 32.3 (clusters of 4 34.2); 16 documents
+// of 8191: a CTA a document and head 32.6 (split in two 43.6).
+Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int G) {
+  const int many = m->dims.dtype == KVR_DTYPE_BF16 ? 12 : 8;
+  int most = 1;
+  for (const auto &x : pages) most = std::max(most, x.first);
+  Deal best{};
+  long long least = -1;
+  for (int W : {many, 4}) {
+    const int per_sm = packed_attn_ctas_per_sm(m->dims.dtype, W);
+    for (int rounds = 1;; rounds += 1 + rounds / 12) {
+      for (int cl = 1; cl <= PACK_CLUSTER; cl *= 2) {
+        const Deal d{W, W * rounds, cl};
+        if (cl > 1 && cl / 2 * d.per >= most) break;  // half the cluster would do
+        long long ctas = 0;
+        for (const auto &x : pages) ctas += (long long)d.parts(x.first) * x.second * G;
+        const long long slots = std::max<long long>(
+            cl, (long long)m->num_sms * per_sm * (cl == 8 ? 15 : cl == 4 ? 19 : 20) / 20);
+        const long long waves = (ctas + slots - 1) / slots;
+        const long long here = std::min<long long>(per_sm, (ctas + m->num_sms - 1) / m->num_sms);
+        const int deep = (std::min(d.per, most) + W - 1) / W, nc = d.parts(most) / cl;
+        const long long t = waves * (520 + deep * (135 + 10 * W * here)) + (cl > 1 ? 90 : 0) +
+                            (nc > 1 ? 310 + 4 * nc : 0);
+        if (least < 0 || t < least) least = t, best = d;
+      }
+      if (W * rounds >= most) break;
+    }
+  }
+  return best;
 }
 
 // The tables of rows at `pos`, built and sent.
@@ -135,7 +171,7 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   const int grp = dm.H / dm.G, M = (int)r->pos.size(), D = (int)r->docs.size();
   std::vector<PackedPart> tiles;  // page1: all of the tile's
   std::vector<PackedRow> rows(M);
-  long long total = 0;
+  std::vector<int> pages;
   int row0 = 0, most = 1;
   for (int d = 0; d < D; ++d) {
     const int R = r->doc_rows[d];
@@ -151,19 +187,25 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
       t.page1 = last < 0 ? 0 : last / KVR_PAGE + 1;
       t.tile = (int)tiles.size();
       tiles.push_back(t);
-      total += t.page1;
+      pages.push_back(t.page1);
       most = std::max(most, t.page1);
     }
     row0 += R;
   }
-  const Deal dl = deal(m, total * dm.G);
+  std::sort(pages.begin(), pages.end());
+  std::vector<std::pair<int, int>> count;  // tiles of so many pages
+  for (int np : pages) {
+    if (count.empty() || count.back().first != np) count.push_back({np, 0});
+    ++count.back().second;
+  }
+  const Deal dl = deal(m, count, dm.G);
   std::vector<PackedPart> parts;
   for (const PackedPart &t : tiles) {
     PackedPart x = t;
     x.slot = (int)parts.size();
-    x.n_parts = std::max(1, (t.page1 + dl.per - 1) / dl.per);
+    x.n_parts = dl.parts(t.page1);
     for (x.part = 0; x.part < x.n_parts; ++x.part) {
-      x.page0 = x.part * dl.per;
+      x.page0 = std::min(t.page1, x.part * dl.per);
       x.page1 = std::min(t.page1, x.page0 + dl.per);
       parts.push_back(x);
     }
@@ -185,6 +227,7 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   r->n_tiles = (int)tiles.size();
   r->max_pages = most;
   r->warps = dl.warps;
+  r->cluster = dl.cluster;
   std::copy(pos, pos + M, r->pos.begin());
   r->sent = true;
   return KVR_OK;
@@ -192,8 +235,10 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
 
 // Room for the partial sums and arrival counts of a launch.
 kvr_status attn_workspace(kvr_model *m, PackedAttnArgs &a, long long parts, long long tiles) {
-  const size_t o = up256(packed_attn_ws_floats(parts, a.G, a.dh) * 4),
-               ml = (size_t)parts * a.G * PACK_VEC * sizeof(float2), cb = (size_t)tiles * a.G * 4;
+  const size_t sums = (size_t)(parts / a.cluster) * a.G,
+               o = up256(sums * PACK_VEC * a.dh * sizeof(float)),
+               ml = sums * PACK_CLUSTER * PACK_VEC * sizeof(float2),
+               cb = (size_t)tiles * a.G * PACK_CLUSTER * sizeof(int);
   if (o + ml > m->pack_ws_bytes)
     KVR_TRY(grow_device(m, m->pack_ws, m->pack_ws_bytes, o + ml, "packed attention workspace"));
   if (cb > m->pack_count_bytes) {
@@ -235,6 +280,7 @@ kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, Pac
   a.parts = r->parts_d;
   a.n_parts = r->n_parts;
   a.warps = r->warps;
+  a.cluster = r->cluster;
   a.settled = r->settled;
   a.n_rows = (int)r->pos.size();
   a.dev_flag = m->dev_flag;
@@ -455,12 +501,13 @@ kvr_status kvr_packed_attention_blocks(kvr_rows *r, int32_t layer, const void *q
   a.blocks = blocks;
   a.n_blocks = n_blocks;
   const long long tiles = (long long)a.n_rows * ((a.grp + PACK_VEC - 1) / PACK_VEC);
-  const Deal dl = deal(m, tiles * a.G * n_blocks);
-  const int per = std::min(dl.per, packed_attn_max_blocks_per_part());
-  a.warps = dl.warps;
-  a.parts_per_row = (n_blocks + per - 1) / per;
-  if (tiles * a.parts_per_row > 0x7FFFFFFF)
+  if (tiles * n_blocks > 0x7FFFFFFF)
     return fail(KVR_E_UNSUPPORTED, "too many rows (%d) for %d blocks each", a.n_rows, n_blocks);
+  Deal dl = deal(m, {{n_blocks, (int)tiles}}, a.G);
+  dl.per = std::min(dl.per, packed_attn_max_blocks_per_part());
+  a.warps = dl.warps;
+  a.cluster = dl.cluster;
+  a.parts_per_row = dl.parts(n_blocks);
   KVR_TRY(attn_workspace(m, a, tiles * a.parts_per_row, tiles));
   if (const char *e = launch_packed_attention(a, m->stream))
     return fail(KVR_E_CUDA, "block attention: %s", e);

@@ -139,6 +139,7 @@ void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, 
 // A tile of the attention is up to 8 query vectors (row * heads per KV head + head) of
 // rows of one document; its pages are dealt to parts, a CTA each.
 constexpr int PACK_VEC = 8;
+constexpr int PACK_CLUSTER = 8;  // parts whose sums meet in shared memory, at most
 struct PackedPart {
   const uint8_t *blocks;  // the document's
   int32_t pages;          // its capacity
@@ -162,21 +163,19 @@ struct PackedAttnArgs {
   const PackedRow *rows;    // device [rows]
   // dense
   const PackedPart *parts;
-  int n_parts, warps;       // packed_attn_warps'
+  int n_parts;
+  int warps, cluster;       // of a CTA, CTAs of a cluster: parts of a tile come in whole clusters
   // sparse: blocks [rows][G][n_blocks]
   const int32_t *blocks;
   int n_rows, n_blocks, parts_per_row;
-  float *ws_o;      // [part][G][PACK_VEC][dh]
-  float2 *ws_ml;    // [part][G][PACK_VEC]
-  int *counters;    // [tile][G], zero between calls
+  float *ws_o;      // [cluster][G][PACK_VEC][dh]
+  float2 *ws_ml;    // [cluster][G][PACK_CLUSTER][PACK_VEC]
+  int *counters;    // [tile][G][PACK_CLUSTER], zero between calls
   int *dev_flag;
   bool settled;     // the tables were sent before the kernel that precedes this one
 };
-// Warps per CTA for `total` (page, KV head) units, and CTAs of an SM.
-int packed_attn_warps(int dtype, long long total, int num_sms);
-int packed_attn_ctas_per_sm(int dtype, int warps);
+int packed_attn_ctas_per_sm(int dtype, int warps);  // CTAs of 4, or 12 (fp32: 8), warps
 int packed_attn_max_blocks_per_part();
-size_t packed_attn_ws_floats(long long n_parts, int G, int dh);
 const char *launch_packed_attention(const PackedAttnArgs &a, cudaStream_t s);
 // Blocks of each (row, KV head): blocks [rows][G][n_blocks].
 const char *launch_packed_select(const PackedAttnArgs &a, int max_pages, int32_t *blocks,
@@ -209,7 +208,7 @@ struct kvr_rows {
   kvr_model *model = nullptr;
   std::vector<kvr_packed *> docs;  // null: freed since
   std::vector<int32_t> doc_rows, pos;
-  int n_parts = 0, n_tiles = 0, max_pages = 0, warps = 0;
+  int n_parts = 0, n_tiles = 0, max_pages = 0, warps = 0, cluster = 0;
   bool sent = false;     // the device holds the tables of pos
   bool settled = false;  // and a kernel was launched behind their upload
   void *mem = nullptr;  // device tables
