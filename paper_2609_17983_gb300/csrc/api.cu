@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "kvr_internal.cuh"
+#include "packed.cuh"
 
 using namespace kvr;
 
@@ -943,6 +944,47 @@ kvr_status grow_device(kvr_model *m, void *&buf, size_t &have, size_t need, cons
 }
 kvr_status synchronize(kvr_model *m) { return sync_model(m); }
 kvr_status flush_uploads(kvr_model *m) { return stage_flush(m); }
+
+bool many_plan(const kvr_model *m, const int32_t *pos, int rows, std::vector<int32_t> &tables,
+               ManyPlan &p) {
+  if (!use_tc_attention(m) || rows < 1) return false;
+  static const CUtensorMap any{};
+  Rows r;
+  r.M = rows;
+  r.tm_kv = &any;  // there will be one
+  const AttnPlan a = make_plan(m, r, pos, nullptr);
+  if (!a.tc5 || a.nb > 60000) return false;  // grid dimensions
+  p.rows = rows;
+  p.n_blocks = a.nb;
+  p.n_pairs = (int)a.pairs.size();
+  p.splits = a.splits;
+  p.block_rows = a.max_rows;
+  p.pages = pos[rows - 1] / KVR_PAGE + 1;
+  tables.insert(tables.end(), a.b.begin(), a.b.end());
+  for (const auto &x : a.pairs) tables.insert(tables.end(), x.begin(), x.end());
+  return true;
+}
+
+kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, const void *q,
+                          const int32_t *pos, void *pages, const int32_t *identity, void *out) {
+  Dims dm = m->dims;
+  dm.L = 1;  // the pages hold one layer
+  CUtensorMap tm;
+  if (!make_tmap_bf16(&tm, pages, p.pages * 2 * dm.G * KVR_PAGE, dm.dh, KVR_PAGE))
+    return fail(KVR_E_CUDA, "tensor map of unpacked pages");
+  Prof pr(m, P_ATTN, (int64_t)p.pages * KVR_PAGE * dm.G * dm.dh * 2 * 2);
+  const char *e =
+      p.n_pairs ? launch_attention_pair(q, pos, tables, p.n_blocks, tables + p.n_blocks, p.n_pairs,
+                                        p.splits, dm, 0, identity, tm, m->attn_ws_o, m->attn_ws_ml,
+                                        out, m->dev_flag, m->stream)
+                : launch_attention_tc5(q, pos, tables, p.n_blocks, p.splits, dm, 0, pages, identity,
+                                       tm, m->attn_ws_o, m->attn_ws_ml, out, m->dev_flag, m->stream);
+  if (!e)
+    e = launch_attention_combine(tables, p.n_blocks, p.block_rows, p.splits, dm, m->attn_ws_o,
+                                 m->attn_ws_ml, out, m->stream);
+  if (e) return fail(KVR_E_CUDA, "attention over unpacked pages: %s", e);
+  return launch_check(m, p.splits > 1 ? 2 : 1);
+}
 }  // namespace kvr
 
 extern "C" {
@@ -989,6 +1031,8 @@ void kvr_model_free(kvr_model *m) {
   dev_free(m->spare_pages);
   dev_free(m->pack_ws);
   dev_free(m->pack_count);
+  dev_free(m->pack_pages);
+  dev_free(m->pack_q);
   dev_free(m->tcw.counters);
   dev_free(m->blocks_d);
   dev_free(m->attn_ws_o);

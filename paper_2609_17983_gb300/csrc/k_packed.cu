@@ -332,6 +332,51 @@ __global__ void __launch_bounds__(2 * DH)
   }
 }
 
+// A CTA per (KV head, page): the block as bf16 pages [page][K, V][G][KVR_PAGE][DH].
+template <int DH>
+__global__ void __launch_bounds__(2 * DH)
+    k_packed_unpack(const PackedView v, int layer, __nv_bfloat16 *pages) {
+  constexpr int NT = 2 * DH, CH = DH / 8, HB = pack_half_bytes(DH);
+  __shared__ __align__(16) uint8_t blk[2 * HB];
+  const int tid = threadIdx.x, g = blockIdx.x, page = blockIdx.y;
+  pdl_trigger();
+  pdl_wait();
+  const uint8_t *src = v.block(layer, g, page);
+  for (int i = tid; i < 2 * HB / 16; i += NT) ((uint4 *)blk)[i] = ((const uint4 *)src)[i];
+  __syncthreads();
+  const int kg = tid / CH, ch = tid % CH;
+  bool bad[4];  // any scale of a row tells
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    bad[j] = blk[pack_k_scale(DH, 4 * kg + j, 0)] == PACK_NAN ||
+             blk[HB + pack_v_scale(DH, 4 * kg + j, 0)] == PACK_NAN;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    const uint8_t *half = blk + kv * HB;
+    uint32_t c[4];
+    if (kv)
+      v_codes_load(half, kg, ch, c);
+    else
+      k_codes_load<DH>(half, kg, ch, c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = kv ? pack_v_scale(DH, 4 * kg + j, ch >> 1)
+                        : pack_k_scale(DH, 4 * kg + j, ch >> 1);
+      __half2 y[4];
+      eight_values(c[j], bad[j] ? (kv ? 0 : PACK_NAN) : half[at], y);
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(y[i]);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+        w[i] = *(const uint32_t *)&b;
+      }
+      *(uint4 *)(pages + ((((size_t)page * 2 + kv) * v.G + g) * KVR_PAGE + 4 * kg + j) * DH +
+                 8 * ch) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
 // ------------------------------------------------------------ block selection
 
 // A CTA per (row, KV head): P_c = sum over the group's heads of max(q, 0), N_c that of
@@ -477,6 +522,16 @@ void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, 
     run(v.dh == 128 ? k_packed_read<128, float> : k_packed_read<64, float>, (float *)k,
         (float *)val);
   }
+}
+
+void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, bool settled,
+                          cudaStream_t s) {
+  auto *kernel = v.dh == 128 ? k_packed_unpack<128> : k_packed_unpack<64>;
+  const dim3 grid(v.G, n_pages);
+  if (settled)
+    launch_pdl(kernel, grid, dim3(2 * v.dh), 0, s, v, layer, (__nv_bfloat16 *)pages);
+  else
+    kernel<<<grid, 2 * v.dh, 0, s>>>(v, layer, (__nv_bfloat16 *)pages);
 }
 
 const char *launch_packed_select(const PackedAttnArgs &a, int max_pages, int32_t *blocks,

@@ -279,6 +279,10 @@ struct kvr_model {
   size_t pack_ws_bytes = 0;
   void *pack_count = nullptr;  // and their arrivals, zero between calls
   size_t pack_count_bytes = 0;
+  void *pack_pages = nullptr;  // a layer's pages of a document, unpacked for many rows
+  size_t pack_pages_bytes = 0;
+  void *pack_q = nullptr;      // their queries, where the caller's rows lie apart
+  size_t pack_q_bytes = 0;
   int *dev_flag = nullptr;     // device error flag (bounded waits)
   kvr::TraceBuf trace{};       // attached device timeline buffer, if any
   kvr::SplitView pending{};    // split tiles of h not yet added (next RMSNorm adds them)

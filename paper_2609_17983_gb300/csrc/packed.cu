@@ -164,6 +164,24 @@ Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int
   return best;
 }
 
+// Whether the rows of a document at `pos` (ascending, >= 0) go by way of unpacked pages: one
+// kernel widens the layer's blocks to bf16 pages, and the tcgen05 attention takes a tile of
+// 128 vectors at a time where the fused kernel takes 8.  By (page, tile of 8 vectors, KV
+// head) units u and positions n the fused kernel takes about 6 + 0.0015 u us (head size
+// 64: 4 + 0.0009 u), the other way 13 + 0.0008 n + 0.00025 u, for every document anew.  40
+// rows over 5000 positions (28 heads) 18 against 20 us, 64 rows 25 against 23; a chunk
+// of 4096 rows over 12345 positions 2993 against 478.
+bool many_rows(const kvr_model *m, const int32_t *pos, int rows, size_t docs) {
+  const Dims &dm = m->dims;
+  if (dm.dtype != KVR_DTYPE_BF16 || rows < 1) return false;
+  const int grp = dm.H / dm.G;
+  long long units = 0;
+  for (int v = 0; v < rows * grp; v += PACK_VEC)
+    units += pos[std::min(rows * grp - 1, v + PACK_VEC - 1) / grp] / KVR_PAGE + 1;
+  const long long n = pos[rows - 1] + 1;
+  return units * dm.G > (docs > 1 ? 5000 : 0) + (dm.dh == 128 ? 5600 + n * 16 / 25 : 6500 + n * 9 / 10);
+}
+
 // The tables of rows at `pos`, built and sent.
 kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   kvr_model *m = r->model;
@@ -172,17 +190,31 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   std::vector<PackedPart> tiles;  // page1: all of the tile's
   std::vector<PackedRow> rows(M);
   std::vector<int> pages;
-  int row0 = 0, most = 1;
+  std::vector<int32_t> tables;
+  std::vector<kvr_rows::Many> many;
+  int row0 = 0, most = 1, many_pages = 0;
   for (int d = 0; d < D; ++d) {
     const int R = r->doc_rows[d];
     const PackedView view = r->docs[d]->view();
     for (int i = row0; i < row0 + R; ++i) rows[i] = PackedRow{view, pos[i], 0};
-    for (int v = 0; v < R * grp; v += PACK_VEC) {
+    int few = R;  // rows that the fused kernel takes: the first ones
+    {
+      const int none = (int)(std::lower_bound(pos + row0, pos + row0 + R, 0) - (pos + row0));
+      kvr_rows::Many x{d, row0 + none, tables.size(), {}};
+      if (many_rows(m, pos + row0 + none, R - none, r->docs.size()) &&
+          many_plan(m, pos + row0 + none, R - none, tables, x.plan)) {
+        few = none;
+        many.push_back(x);
+        many_pages = std::max(many_pages, x.plan.pages);
+        most = std::max(most, x.plan.pages);
+      }
+    }
+    for (int v = 0; v < few * grp; v += PACK_VEC) {
       PackedPart t{};
       t.blocks = view.blocks;
       t.pages = view.pages;
       t.vec0 = row0 * grp + v;
-      t.nvec = std::min(PACK_VEC, R * grp - v);
+      t.nvec = std::min(PACK_VEC, few * grp - v);
       const int last = pos[(t.vec0 + t.nvec - 1) / grp];  // positions ascend
       t.page1 = last < 0 ? 0 : last / KVR_PAGE + 1;
       t.tile = (int)tiles.size();
@@ -211,11 +243,14 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
     }
   }
   const size_t o_row = up256(parts.size() * sizeof(PackedPart)),
-               o_pos = up256(o_row + M * sizeof(PackedRow)), bytes = up256(o_pos + M * 4ull);
+               o_pos = up256(o_row + M * sizeof(PackedRow)), o_many = up256(o_pos + M * 4ull),
+               o_id = up256(o_many + tables.size() * 4), bytes = up256(o_id + many_pages * 4ull);
   std::vector<char> host(bytes);
   memcpy(host.data(), parts.data(), parts.size() * sizeof(PackedPart));
   memcpy(host.data() + o_row, rows.data(), M * sizeof(PackedRow));
   memcpy(host.data() + o_pos, pos, M * 4ull);
+  memcpy(host.data() + o_many, tables.data(), tables.size() * 4);
+  for (int i = 0; i < many_pages; ++i) ((int32_t *)(host.data() + o_id))[i] = i;
   r->sent = r->settled = false;
   KVR_TRY(grow_device(m, r->mem, r->mem_bytes, bytes, "query rows"));
   KVR_TRY(upload_words(m, r->mem, host.data(), bytes / 4));
@@ -223,6 +258,9 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   r->parts_d = (PackedPart *)base;
   r->rows_d = (PackedRow *)(base + o_row);
   r->pos_d = (int32_t *)(base + o_pos);
+  r->many_d = (int32_t *)(base + o_many);
+  r->identity_d = (int32_t *)(base + o_id);
+  r->many = std::move(many);
   r->n_parts = (int)parts.size();
   r->n_tiles = (int)tiles.size();
   r->max_pages = most;
@@ -464,11 +502,33 @@ kvr_status kvr_packed_attention(kvr_rows *r, int32_t layer, const void *q, int32
   kvr_model *m = r->model;
   KVR_TRY(check_device_ptr(m, out, "out"));
   a.out = out;
-  KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles));
-  if (const char *e = launch_packed_attention(a, m->stream))
-    return fail(KVR_E_CUDA, "packed attention: %s", e);
-  KVR_TRY(launched(m, 1, "packed attention"));
-  r->settled = true;
+  if (r->n_parts) {
+    KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles));
+    if (const char *e = launch_packed_attention(a, m->stream))
+      return fail(KVR_E_CUDA, "packed attention: %s", e);
+    KVR_TRY(launched(m, 1, "packed attention"));
+    r->settled = true;
+  }
+  const Dims &dm = m->dims;
+  const size_t row_b = (size_t)dm.H * dm.dh * dm.es(), page_b = (size_t)2 * dm.G * KVR_PAGE * dm.dh * 2;
+  for (const kvr_rows::Many &x : r->many) {
+    KVR_TRY(grow_device(m, m->pack_pages, m->pack_pages_bytes, x.plan.pages * page_b,
+                        "unpacked pages"));
+    const char *qr = (const char *)q + (size_t)x.row0 * ldq * dm.es();
+    if (ldq != dm.H * dm.dh) {  // the kernels take rows side by side
+      KVR_TRY(grow_device(m, m->pack_q, m->pack_q_bytes, x.plan.rows * row_b, "query rows"));
+      if (cudaMemcpy2DAsync(m->pack_q, row_b, qr, ldq * dm.es(), row_b, x.plan.rows,
+                            cudaMemcpyDeviceToDevice, m->stream) != cudaSuccess)
+        return fail(KVR_E_CUDA, "query rows");
+      qr = (const char *)m->pack_q;
+    }
+    launch_packed_unpack(r->docs[x.doc]->view(), layer, x.plan.pages, m->pack_pages, r->settled,
+                         m->stream);
+    KVR_TRY(launched(m, 1, "unpack"));
+    r->settled = true;
+    KVR_TRY(many_attention(m, x.plan, (const int4 *)(r->many_d + x.table), qr, r->pos_d + x.row0,
+                           m->pack_pages, r->identity_d, (char *)out + x.row0 * row_b));
+  }
   return KVR_OK;
 }
 

@@ -188,6 +188,21 @@ kvr_status grow_device(kvr_model *m, void *&buf, size_t &have, size_t need, cons
 kvr_status synchronize(kvr_model *m);
 kvr_status flush_uploads(kvr_model *m);
 
+// Many rows of one document over unpacked pages: the plan of the tensor-core attention
+// for rows at ascending positions >= 0 (its tables, int4, to be sent to the device), and
+// its launch on pages [page][K, V][G][KVR_PAGE][dh] of one layer.
+struct ManyPlan {
+  int rows = 0, n_blocks = 0, n_pairs = 0, splits = 1, block_rows = 0, pages = 0;
+};
+bool many_plan(const kvr_model *m, const int32_t *pos, int rows, std::vector<int32_t> &tables,
+               ManyPlan &p);
+kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, const void *q,
+                          const int32_t *pos, void *pages, const int32_t *identity, void *out);
+// The first n_pages blocks of a layer as such pages (bf16).  A key row stored as NaN, or
+// whose value row is, becomes NaN; NaN value rows become zero.
+void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, bool settled,
+                          cudaStream_t s);
+
 }  // namespace kvr
 
 // A document's packed cache.
@@ -205,6 +220,13 @@ struct kvr_packed {
 
 // Query rows over packed documents: the tables of a pass, used by every layer of it.
 struct kvr_rows {
+  struct Many {  // rows [row0, row0 + plan.rows) of a document, by way of unpacked pages
+    int doc, row0;
+    size_t table;  // int32 words into many_d
+    kvr::ManyPlan plan;
+  };
+  std::vector<Many> many;
+  int32_t *many_d = nullptr, *identity_d = nullptr;
   kvr_model *model = nullptr;
   std::vector<kvr_packed *> docs;  // null: freed since
   std::vector<int32_t> doc_rows, pos;

@@ -149,7 +149,7 @@ def test_store_many_scattered_rows(models):
     doc.close()
 
 
-def bound(dtype, ref, vmax, smax):
+def bound(dtype, ref, vmax, smax, weight_bits=11):
     """What the roundings allow.  bf16: the output to 8 bits (off by at most 2^-8 of itself), the
     weights to 11 (so at most 2^-11 of the largest value), the scores' and exponentials'
     fp32.  fp32: weights to 22 bits; a score is a sum of 8 (head size 128) products of fragments in two parts,
@@ -158,14 +158,15 @@ def bound(dtype, ref, vmax, smax):
     that of the largest value."""
     delta = 2.0 ** -19 + 16 * 2.0 ** -23 * smax
     if dtype == "bf16":
-        return 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + 2 * delta)[..., None] * vmax[..., None]
+        return (2.0 ** -8 * np.abs(ref) +
+                (2.0 ** -weight_bits + 2 * delta)[..., None] * vmax[..., None])
     return (2 * delta * vmax)[..., None] + 2.0 ** -24 * np.abs(ref)
 
 
-def check(got, q, pos, k, v, dtype, blocks=None):
+def check(got, q, pos, k, v, dtype, blocks=None, weight_bits=11):
     ref, vmax, smax = pp.attention(q, pos, k, v, blocks)
     assert np.array_equal(np.isnan(got), np.isnan(ref))
-    err = np.abs(got - ref) - bound(dtype, ref, vmax, smax)
+    err = np.abs(got - ref) - bound(dtype, ref, vmax, smax, weight_bits)
     assert not (err > 0).any(), float(np.nanmax(err))
 
 
@@ -223,6 +224,46 @@ def test_attention_several_documents_and_moves(models, dtype):
                       dtype)
             i += len(p)
     r.close()
+
+
+@pytest.mark.parametrize("shape,n,R,spread", [("dh64", 4000, 1201, True), ("dh128", 2000, 300, False),
+                                              ("dh128", 2049, 501, True)])
+def test_attention_many_rows(models, shape, n, R, spread):
+    """Rows that go by way of unpacked pages (their weights are rounded to bf16's 8 bits): odd
+    lengths, rows that see nothing, a second document with few rows, q rows apart, NaN."""
+    dh, H, G = SHAPES[shape]
+    m = models(shape, "bf16")
+    k, v = rows(n, n, 2, G, dh, "bf16"), rows(n + 1, n, 2, G, dh, "bf16")
+    k[n - 10, :, 0, 7], v[n - 5, :, G - 1, 3] = float("nan"), float("inf")
+    doc = m.packed(n + 1)
+    doc.write(np.arange(n), k, v)
+    k, v = pp.stored(f64(k)), pp.stored(f64(v))
+    small, ks, vs = document(m, 5, 100, shape, "bf16")
+    pos = np.linspace(0, n - 1, R).astype(int) if spread else np.arange(n - R, n)
+    pos[:3] = -1
+    r = m.rows([(small, [50]), (doc, pos)])
+    wide = torch.randn((R + 1, H + 2 * G, dh), device="cuda").bfloat16()
+    q = wide[:, :H]
+    out = torch.full((R + 1, H, dh), float("nan"), dtype=torch.bfloat16, device="cuda")
+    before = m.launches()
+    r.attention(1, q, out)
+    assert m.launches() - before >= 3  # the small document's, the unpacking, the attention
+    check(f64(out[:1]), f64(q[:1]), np.array([50]), ks[:, 1], vs[:, 1], "bf16")
+    check(f64(out[1:]), f64(q[1:]), pos, k[:, 1], v[:, 1], "bf16", weight_bits=8)
+    assert (out[1:4] == 0).all()
+    again = torch.empty_like(out)
+    r.attention(1, q.contiguous(), again)
+    assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(again))
+    # the block lists of such rows are the fused kernel's
+    blocks = torch.empty((R + 1, G, 3), dtype=torch.int32, device="cuda")
+    r.select(1, q, blocks)
+    r.attention(1, q, again, blocks=blocks)
+    some = np.r_[1, 5, R - 20, R]  # row 1: a row that sees nothing
+    b = blocks.cpu().numpy()[some]
+    assert np.array_equal(b, pp.select(f64(q[some]), pos[some - 1], k[:, 1], 3))
+    check(f64(again[some]), f64(q[some]), pos[some - 1], k[:, 1], v[:, 1], "bf16", b)
+    r.close()
+    doc.close()
 
 
 def test_attention_rows_apart_sizes_and_streams(models):
