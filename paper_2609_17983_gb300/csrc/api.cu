@@ -966,7 +966,7 @@ bool many_plan(const kvr_model *m, const int32_t *pos, int rows, std::vector<int
 }
 
 kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, const void *q,
-                          const int32_t *pos, void *pages, const int32_t *identity, void *out) {
+                          const float *q_scale, const int32_t *pos, void *pages, const int32_t *identity, void *out) {
   Dims dm = m->dims;
   dm.L = 1;  // the pages hold one layer
   CUtensorMap tm;
@@ -976,9 +976,10 @@ kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, c
   const char *e =
       p.n_pairs ? launch_attention_pair(q, pos, tables, p.n_blocks, tables + p.n_blocks, p.n_pairs,
                                         p.splits, dm, 0, identity, tm, m->attn_ws_o, m->attn_ws_ml,
-                                        out, m->dev_flag, m->stream)
+                                        out, m->dev_flag, m->stream, nullptr, nullptr, q_scale)
                 : launch_attention_tc5(q, pos, tables, p.n_blocks, p.splits, dm, 0, pages, identity,
-                                       tm, m->attn_ws_o, m->attn_ws_ml, out, m->dev_flag, m->stream);
+                                       tm, m->attn_ws_o, m->attn_ws_ml, out, m->dev_flag, m->stream,
+                                       nullptr, nullptr, NO_TAIL, 0, q_scale);
   if (!e)
     e = launch_attention_combine(tables, p.n_blocks, p.block_rows, p.splits, dm, m->attn_ws_o,
                                  m->attn_ws_ml, out, m->stream);

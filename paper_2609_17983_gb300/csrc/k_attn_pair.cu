@@ -54,8 +54,9 @@ constexpr uint32_t TMEM_COLS = 512;  // S0, S1 (128 columns each; P over the fir
 constexpr float RESCALE_LOG2 = 8.f;  // headroom of the reference maximum (P <= 2^8)
 
 struct PairParams {
-  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE
+  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE (HALF: halves)
   float qk_scale;          // log2(e) / sqrt(dh): scores into the log2 domain
+  const float *q_scale;    // HALF: [M][H], what q was divided by
   const int32_t *pos;      // [M] ascending per document
   const int4 *blocks;      // tiles: (row0, nrows, kmax, doc)
   const int4 *pairs;       // (first tile, tiles: 1 or 2, kmax of the pair, doc)
@@ -97,6 +98,11 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return *(uint32_t *)&v;
 }
 
+__device__ __forceinline__ uint32_t pack2_half(float lo, float hi) {
+  __half2 v = __floats2half2_rn(lo, hi);
+  return *(uint32_t *)&v;
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -118,7 +124,7 @@ __device__ __forceinline__ void add2(float &a0, float &a1, float b0, float b1) {
       : "f"(b0), "f"(b1));
 }
 
-template <int DH>
+template <int DH, bool HALF>
 __global__ void __launch_bounds__(NT, 1)
     k_attn_pair(const __grid_constant__ CUtensorMap tm_kv, const PairParams p) {
   constexpr int HALVES = DH / 64;                    // 128-byte column blocks of a row
@@ -249,7 +255,7 @@ __global__ void __launch_bounds__(NT, 1)
     // The whole warp walks the loop and one elected lane issues, so the
     // operands stay in uniform registers.  A group of the ring (V of a step, K
     // of the next) is used in one go and released by one commit.
-    const uint32_t id_s = idesc_bf16(QV, CH), id_o = idesc_bf16(QV, DH, 1);
+    const uint32_t id_s = idesc_16(HALF, QV, CH), id_o = idesc_16(HALF, QV, DH, 1);
     // descriptors built once; a slot, column block or K slice only moves the
     // start address (the descriptor's low field, address / 16)
     const uint64_t dq0 = sw128_desc(sQ), dk0 = sw128_desc(sKV),
@@ -356,6 +362,8 @@ __global__ void __launch_bounds__(NT, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_full);
     }
+    float qk_scale = p.qk_scale;
+    if (HALF && real) qk_scale *= p.q_scale[(size_t)row * p.H + hh];
     float m = -INFINITY, l = 0.f;  // reference maximum, this half's sum of exponentials
     bool dead = false;             // warp-uniform: a wait ran out
     for (int i = 0; i < n; ++i) {
@@ -390,7 +398,7 @@ __global__ void __launch_bounds__(NT, 1)
           for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(s[j]));
         }
         // the scale is positive: the scaled maximum is the maximum scaled
-        ms = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.qk_scale;
+        ms = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * qk_scale;
       }
       // Either half of a row of these 32 above its reference's headroom (the
       // first step, whose reference is -inf, always).
@@ -429,10 +437,10 @@ __global__ void __launch_bounds__(NT, 1)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             float a, b;
-            fma2(a, b, s[16 * h + 2 * j], s[16 * h + 2 * j + 1], p.qk_scale, nm);
+            fma2(a, b, s[16 * h + 2 * j], s[16 * h + 2 * j + 1], qk_scale, nm);
             a = ex2(a);
             b = ex2(b);
-            w[j] = pack2(a, b);
+            w[j] = HALF ? pack2_half(a, b) : pack2(a, b);
             add2(sum[2 * (j & 1)], sum[2 * (j & 1) + 1], a, b);
           }
           tmem_st8_nowait(tS + 16 * k + 8 * h, w);  // below the scores yet to be read
@@ -515,13 +523,13 @@ __global__ void __launch_bounds__(NT, 1)
   ts.finish();
 }
 
-template <int DH>
+template <int DH, bool HALF>
 const char *run(const CUtensorMap &tm, const PairParams &p, int n_pairs, cudaStream_t s) {
   constexpr size_t smem = 1024 + (2 * QV + NSLOT * CH) * (size_t)DH * 2;
   static PerDevice<size_t> limit;
-  if (const char *e = smem_opt_in(limit, k_attn_pair<DH>, smem)) return e;
+  if (const char *e = smem_opt_in(limit, k_attn_pair<DH, HALF>, smem)) return e;
   dim3 grid(p.n_splits, p.G, n_pairs);
-  launch_pdl(k_attn_pair<DH>, grid, NT, smem, s, tm, p);
+  launch_pdl(k_attn_pair<DH, HALF>, grid, NT, smem, s, tm, p);
   cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
@@ -533,11 +541,12 @@ const char *launch_attention_pair(const void *q, const int32_t *pos, const int4 
                                   const Dims &dm, int layer, const int32_t *table,
                                   const CUtensorMap &tm_kv, float *ws_o, float2 *ws_ml, void *out,
                                   int *dev_flag, cudaStream_t s, const KVView *views,
-                                  const CUtensorMap *tmaps) {
+                                  const CUtensorMap *tmaps, const float *q_scale) {
   if (n_pairs <= 0) return nullptr;
   if ((views == nullptr) != (tmaps == nullptr)) return "document views without tensor maps";
   PairParams p{};
   p.q = (const __nv_bfloat16 *)q;
+  p.q_scale = q_scale;
   p.qk_scale = (float)(1.4426950408889634 / std::sqrt((double)dm.dh));
   p.pos = pos;
   p.blocks = blocks;
@@ -556,8 +565,10 @@ const char *launch_attention_pair(const void *q, const int32_t *pos, const int4 
   p.ws_ml = ws_ml;
   p.out = (__nv_bfloat16 *)out;
   p.dev_flag = dev_flag;
-  if (dm.dh == 128) return run<128>(tm_kv, p, n_pairs, s);
-  if (dm.dh == 64) return run<64>(tm_kv, p, n_pairs, s);
+  if (dm.dh == 128)
+    return q_scale ? run<128, true>(tm_kv, p, n_pairs, s) : run<128, false>(tm_kv, p, n_pairs, s);
+  if (dm.dh == 64)
+    return q_scale ? run<64, true>(tm_kv, p, n_pairs, s) : run<64, false>(tm_kv, p, n_pairs, s);
   return "head_dim not supported";
 }
 

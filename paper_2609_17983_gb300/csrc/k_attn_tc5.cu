@@ -69,8 +69,9 @@ constexpr float RESCALE_LOG2 = 8.f;  // headroom of the reference maximum (P <= 
 constexpr int KV_STAGES = 4;
 
 struct Attn5Params {
-  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE
+  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE (HALF: halves)
   float qk_scale;          // log2(e) / sqrt(dh): scores into the log2 domain
+  const float *q_scale;    // HALF: [M][H], what q was divided by
   const int32_t *pos;      // [M] ascending (one document)
   const int4 *blocks;      // (row0, nrows, kmax, doc)
   const __nv_bfloat16 *pages;  // the cache's page pool (one document)
@@ -118,13 +119,18 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return *(uint32_t *)&v;
 }
 
+__device__ __forceinline__ uint32_t pack2_half(float lo, float hi) {
+  __half2 v = __floats2half2_rn(lo, hi);
+  return *(uint32_t *)&v;
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
-template <int DH>
+template <int DH, bool HALF>
 __global__ void __launch_bounds__(NT5, 1)
     k_attn_tc5(const __grid_constant__ CUtensorMap tm_kv, const Attn5Params p) {
   constexpr int HALVES = DH / 64;           // 128-byte column blocks of a row
@@ -263,7 +269,7 @@ __global__ void __launch_bounds__(NT5, 1)
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA
     if (lane == 0) {
-      const uint32_t id_s = idesc_bf16(QV, CH), id_o = idesc_bf16(QV, DH, 1);
+      const uint32_t id_s = idesc_16(HALF, QV, CH), id_o = idesc_16(HALF, QV, DH, 1);
       // This one thread's issue path bounds the chunk rate (it shares its SM
       // sub-partition with four softmax warps), so the shared-memory
       // descriptors are built once: a stage, a 64-wide column block or a
@@ -361,6 +367,9 @@ __global__ void __launch_bounds__(NT5, 1)
     constexpr int HK = CH / SMW;  // keys of this thread per chunk
     constexpr int OC = DH / SMW;  // O columns of this thread
     const int pv = spos[v];
+    float qk_scale = p.qk_scale;
+    if (HALF && v < mq)
+      qk_scale *= p.q_scale[(size_t)(row0 + v / p.grp) * p.H + g * p.grp + v % p.grp];
     float m = -INFINITY, l = 0.f;  // reference maximum, this part's sum of exponentials
     bool dead = false;             // warp-uniform: a wait ran out
     for (int i = 0; i < nch; ++i) {
@@ -388,14 +397,14 @@ __global__ void __launch_bounds__(NT5, 1)
         if (unmasked) {
 #pragma unroll
           for (int j = 0; j < HK; ++j) {
-            const float x = __uint_as_float(sr[j]) * p.qk_scale;
+            const float x = __uint_as_float(sr[j]) * qk_scale;
             sr[j] = __float_as_uint(x);
             t[j] = x;
           }
         } else {
 #pragma unroll
           for (int j = 0; j < HK; ++j) {
-            const float x = __uint_as_float(sr[j]) * p.qk_scale;
+            const float x = __uint_as_float(sr[j]) * qk_scale;
             sr[j] = __float_as_uint(x);
             t[j] = key0 + j <= pv ? x : -INFINITY;
           }
@@ -452,7 +461,8 @@ __global__ void __launch_bounds__(NT5, 1)
       {  // P in bf16 pairs: this part's HK keys are HK / 2 columns of buffer b
         uint32_t w[HK / 2];
 #pragma unroll
-        for (int j = 0; j < HK / 2; ++j) w[j] = pack2(e[2 * j], e[2 * j + 1]);
+        for (int j = 0; j < HK / 2; ++j) 
+          w[j] = HALF ? pack2_half(e[2 * j], e[2 * j + 1]) : pack2(e[2 * j], e[2 * j + 1]);
 #pragma unroll
         for (int q = 0; q < HK / 16; ++q)
           tmem_st8_nowait(tl + T_P + b * (CH / 2) + part * (HK / 2) + q * 8, w + 8 * q);
@@ -547,13 +557,13 @@ constexpr size_t smem_bytes() {
   return 1024 + KV_STAGES * 2 * (size_t)CH * 128 * (DH / 64);
 }
 
-template <int DH>
+template <int DH, bool HALF>
 const char *run(const CUtensorMap &tm, const Attn5Params &p, cudaStream_t s) {
   constexpr size_t smem = smem_bytes<DH>();
   static PerDevice<size_t> limit;
-  if (const char *e = smem_opt_in(limit, k_attn_tc5<DH>, smem)) return e;
+  if (const char *e = smem_opt_in(limit, k_attn_tc5<DH, HALF>, smem)) return e;
   dim3 grid(p.n_splits, p.G, p.n_blocks);
-  launch_pdl(k_attn_tc5<DH>, grid, NT5, smem, s, tm, p);
+  launch_pdl(k_attn_tc5<DH, HALF>, grid, NT5, smem, s, tm, p);
   cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
@@ -570,7 +580,8 @@ const char *launch_attention_tc5(const void *q, const int32_t *pos, const int4 *
                                  const void *pages, const int32_t *table, const CUtensorMap &tm_kv,
                                  float *ws_o, float2 *ws_ml, void *out, int *dev_flag,
                                  cudaStream_t s, const KVView *views,
-                                 const CUtensorMap *tmaps, int tail_page, int tail_docs) {
+                                 const CUtensorMap *tmaps, int tail_page, int tail_docs,
+                                 const float *q_scale) {
   if (n_blocks <= 0) return nullptr;
   if ((views == nullptr) != (tmaps == nullptr)) return "document views without tensor maps";
   if (!views && tail_page != NO_TAIL) return "a tail without document views";
@@ -580,6 +591,7 @@ const char *launch_attention_tc5(const void *q, const int32_t *pos, const int4 *
   p.tail_page = tail_page;
   p.tail_docs = tail_docs;
   p.q = (const __nv_bfloat16 *)q;
+  p.q_scale = q_scale;
   p.qk_scale = (float)(1.4426950408889634 / std::sqrt((double)dm.dh));
   p.pos = pos;
   p.blocks = blocks;
@@ -596,8 +608,8 @@ const char *launch_attention_tc5(const void *q, const int32_t *pos, const int4 *
   p.ws_ml = ws_ml;
   p.out = (__nv_bfloat16 *)out;
   p.dev_flag = dev_flag;
-  if (dm.dh == 128) return run<128>(tm_kv, p, s);
-  if (dm.dh == 64) return run<64>(tm_kv, p, s);
+  if (dm.dh == 128) return q_scale ? run<128, true>(tm_kv, p, s) : run<128, false>(tm_kv, p, s);
+  if (dm.dh == 64) return q_scale ? run<64, true>(tm_kv, p, s) : run<64, false>(tm_kv, p, s);
   return "head_dim not supported";
 }
 

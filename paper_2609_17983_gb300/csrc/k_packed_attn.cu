@@ -249,12 +249,9 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     }
     a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
     a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-    // largest magnitude to [2^8, 2^9); what that leaves below a half's range is below
-    // 2^-32 of it
-    const int e = min(max((int)(__float_as_uint(a) >> 23) - 127, -100), 126) - 8;
-    const float down = __uint_as_float((uint32_t)(127 - e) << 23),
-                upf = __uint_as_float((uint32_t)(127 + e) << 23);
-    qscale = upf * p.scale;
+    const int e = pack_q_exponent(a);
+    const float down = pack_exp2(-e);
+    qscale = pack_exp2(e) * p.scale;
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
 #pragma unroll

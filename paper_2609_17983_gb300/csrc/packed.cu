@@ -165,7 +165,7 @@ Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int
 }
 
 // Whether the rows of a document at `pos` (ascending, >= 0) go by way of unpacked pages: one
-// kernel widens the layer's blocks to bf16 pages, and the tcgen05 attention takes a tile of
+// kernel widens the layer's blocks to pages of halves, and the tcgen05 attention takes a tile of
 // 128 vectors at a time where the fused kernel takes 8.  By (page, tile of 8 vectors, KV
 // head) units u and positions n the fused kernel takes about 6 + 0.0015 u us (head size
 // 64: 4 + 0.0009 u), the other way 13 + 0.0008 n + 0.00025 u, for every document anew.  40
@@ -514,20 +514,18 @@ kvr_status kvr_packed_attention(kvr_rows *r, int32_t layer, const void *q, int32
   for (const kvr_rows::Many &x : r->many) {
     KVR_TRY(grow_device(m, m->pack_pages, m->pack_pages_bytes, x.plan.pages * page_b,
                         "unpacked pages"));
-    const char *qr = (const char *)q + (size_t)x.row0 * ldq * dm.es();
-    if (ldq != dm.H * dm.dh) {  // the kernels take rows side by side
-      KVR_TRY(grow_device(m, m->pack_q, m->pack_q_bytes, x.plan.rows * row_b, "query rows"));
-      if (cudaMemcpy2DAsync(m->pack_q, row_b, qr, ldq * dm.es(), row_b, x.plan.rows,
-                            cudaMemcpyDeviceToDevice, m->stream) != cudaSuccess)
-        return fail(KVR_E_CUDA, "query rows");
-      qr = (const char *)m->pack_q;
-    }
-    launch_packed_unpack(r->docs[x.doc]->view(), layer, x.plan.pages, m->pack_pages, r->settled,
-                         m->stream);
+    const size_t q_b = up256(x.plan.rows * row_b);
+    KVR_TRY(grow_device(m, m->pack_q, m->pack_q_bytes, q_b + (size_t)x.plan.rows * dm.H * 4,
+                        "query rows"));
+    float *q_scale = (float *)((char *)m->pack_q + q_b);
+    launch_packed_unpack(r->docs[x.doc]->view(), layer, x.plan.pages, m->pack_pages,
+                         (const char *)q + (size_t)x.row0 * ldq * dm.es(), ldq, dm.H, x.plan.rows,
+                         m->pack_q, q_scale, r->settled, m->stream);
     KVR_TRY(launched(m, 1, "unpack"));
     r->settled = true;
-    KVR_TRY(many_attention(m, x.plan, (const int4 *)(r->many_d + x.table), qr, r->pos_d + x.row0,
-                           m->pack_pages, r->identity_d, (char *)out + x.row0 * row_b));
+    KVR_TRY(many_attention(m, x.plan, (const int4 *)(r->many_d + x.table), m->pack_q, q_scale,
+                           r->pos_d + x.row0, m->pack_pages, r->identity_d,
+                           (char *)out + x.row0 * row_b));
   }
   return KVR_OK;
 }

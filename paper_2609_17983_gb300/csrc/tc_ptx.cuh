@@ -137,6 +137,11 @@ __device__ __forceinline__ uint32_t idesc_bf16(int m, int n, int b_mn = 0) {
          ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
+// The same with A and B both halves (half) or both bf16.
+__device__ __forceinline__ uint32_t idesc_16(bool half, int m, int n, int b_mn = 0) {
+  return idesc_bf16(m, n, b_mn) & (half ? ~((1u << 7) | (1u << 10)) : ~0u);
+}
+
 __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc,
                                          uint32_t accumulate) {
   asm volatile(

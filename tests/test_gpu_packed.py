@@ -149,7 +149,7 @@ def test_store_many_scattered_rows(models):
     doc.close()
 
 
-def bound(dtype, ref, vmax, smax, weight_bits=11):
+def bound(dtype, ref, vmax, smax):
     """What the roundings allow.  bf16: the output to 8 bits (off by at most 2^-8 of itself), the
     weights to 11 (so at most 2^-11 of the largest value), the scores' and exponentials'
     fp32.  fp32: weights to 22 bits; a score is a sum of 8 (head size 128) products of fragments in two parts,
@@ -159,14 +159,14 @@ def bound(dtype, ref, vmax, smax, weight_bits=11):
     delta = 2.0 ** -19 + 16 * 2.0 ** -23 * smax
     if dtype == "bf16":
         return (2.0 ** -8 * np.abs(ref) +
-                (2.0 ** -weight_bits + 2 * delta)[..., None] * vmax[..., None])
+                (2.0 ** -11 + 2 * delta)[..., None] * vmax[..., None])
     return (2 * delta * vmax)[..., None] + 2.0 ** -24 * np.abs(ref)
 
 
-def check(got, q, pos, k, v, dtype, blocks=None, weight_bits=11):
+def check(got, q, pos, k, v, dtype, blocks=None):
     ref, vmax, smax = pp.attention(q, pos, k, v, blocks)
     assert np.array_equal(np.isnan(got), np.isnan(ref))
-    err = np.abs(got - ref) - bound(dtype, ref, vmax, smax, weight_bits)
+    err = np.abs(got - ref) - bound(dtype, ref, vmax, smax)
     assert not (err > 0).any(), float(np.nanmax(err))
 
 
@@ -229,7 +229,7 @@ def test_attention_several_documents_and_moves(models, dtype):
 @pytest.mark.parametrize("shape,n,R,spread", [("dh64", 4000, 1201, True), ("dh128", 2000, 300, False),
                                               ("dh128", 2049, 501, True)])
 def test_attention_many_rows(models, shape, n, R, spread):
-    """Rows that go by way of unpacked pages (their weights are rounded to bf16's 8 bits): odd
+    """Rows that go by way of unpacked pages: odd
     lengths, rows that see nothing, a second document with few rows, q rows apart, NaN."""
     dh, H, G = SHAPES[shape]
     m = models(shape, "bf16")
@@ -249,7 +249,7 @@ def test_attention_many_rows(models, shape, n, R, spread):
     r.attention(1, q, out)
     assert m.launches() - before >= 3  # the small document's, the unpacking, the attention
     check(f64(out[:1]), f64(q[:1]), np.array([50]), ks[:, 1], vs[:, 1], "bf16")
-    check(f64(out[1:]), f64(q[1:]), pos, k[:, 1], v[:, 1], "bf16", weight_bits=8)
+    check(f64(out[1:]), f64(q[1:]), pos, k[:, 1], v[:, 1], "bf16")
     assert (out[1:4] == 0).all()
     again = torch.empty_like(out)
     r.attention(1, q.contiguous(), again)
