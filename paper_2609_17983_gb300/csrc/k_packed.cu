@@ -2,19 +2,23 @@
 // written, reading them back, and selecting blocks by their bounds.
 #include <math.h>
 
+#include <type_traits>
+
 #include "packed.cuh"
 
 namespace kvr {
 namespace {
 
-// The rows [r0, r1) of segment seg and their page.
+// The rows [r0, r1) of segment seg and their page; the row of a slot of it, or -1.
 struct Segment {
   int page, r0, r1;
 };
-__device__ __forceinline__ int position(const PackedRows &r, int i) {
-  return r.first >= 0 ? r.first + i : r.pos_d ? r.pos_d[i] : r.pos[i];
-}
-__device__ __forceinline__ Segment segment(const PackedRows &r, int seg) {
+__device__ __forceinline__ int position(const PackedRun &r, int i) { return r.pos_d[i]; }
+__device__ __forceinline__ int position(const PackedList &r, int i) { return r.pos[i]; }
+__device__ __forceinline__ int start(const PackedRun &r, int s) { return r.pos_d[r.n + s]; }
+__device__ __forceinline__ int start(const PackedList &r, int s) { return r.seg[s]; }
+template <class Rows>
+__device__ __forceinline__ Segment segment(const Rows &r, int seg) {
   Segment s;
   if (r.first >= 0) {
     s.page = r.first / KVR_PAGE + seg;
@@ -22,25 +26,75 @@ __device__ __forceinline__ Segment segment(const PackedRows &r, int seg) {
     s.r1 = min(r.n, (s.page + 1) * KVR_PAGE - r.first);
     return s;
   }
-  s.r0 = r.pos_d ? r.pos_d[r.n + seg] : r.seg[seg];
-  s.r1 = r.pos_d ? r.pos_d[r.n + seg + 1] : r.seg[seg + 1];
+  s.r0 = start(r, seg);
+  s.r1 = start(r, seg + 1);
   s.page = position(r, s.r0) / KVR_PAGE;
   return s;
 }
+// Rows of the slots 4 kg .. 4 kg + 3 (every thread of the CTA calls it; row_of: shared
+// [KVR_PAGE], used for lists).
+template <class Rows>
+__device__ __forceinline__ void rows_of_slots(const Rows &r, const Segment &s, int *row_of, int kg,
+                                              int *rr) {
+  if (r.first >= 0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = s.page * KVR_PAGE + 4 * kg + j - r.first;
+      rr[j] = i >= s.r0 && i < s.r1 ? i : -1;
+    }
+    return;
+  }
+  if (threadIdx.x < KVR_PAGE) row_of[threadIdx.x] = -1;
+  __syncthreads();
+  for (int i = s.r0 + threadIdx.x; i < s.r1; i += blockDim.x)
+    row_of[position(r, i) % KVR_PAGE] = i;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) rr[j] = row_of[4 * kg + j];
+}
 
-// Eight entries of a row.
+// The larger of two unsigned 16-bit numbers, twice.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Eight entries of a row: loaded, the bits of their largest magnitude as a float
+// (infinities and NaN lie above all others), a group's scale, the codes under a
+// scale s.
 template <typename T>
 struct Eight;
 template <>
 struct Eight<__nv_bfloat16> {
-  static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float *x) {
-    const uint4 u = __ldcs((const uint4 *)p);
+  uint4 u;
+  __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = __ldcs((const uint4 *)p); }
+  // largest magnitudes of the even entries (low half) and of the odd ones
+  __device__ __forceinline__ uint32_t magnitudes() const {
+    return max_u16x2(max_u16x2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu),
+                     max_u16x2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu));
+  }
+  __device__ __forceinline__ uint32_t magnitude() const {
+    const uint32_t m = magnitudes();
+    return max(m & 0xFFFF0000u, m << 16);
+  }
+  static __device__ __forceinline__ uint32_t scale_code(float a) { return pack_scale_code_bf16(a); }
+  // x / s on the grid of the codes.  With r a reciprocal of the four-bit s, off by 2^-22
+  // at most, x r + 768 rounds to whole steps of 2^-14, far above r's error and far below
+  // the distance of an eight-bit x from a midpoint of the codes (at least 2^-10 where it
+  // is not one), so ties are ties and everything else keeps its side.
+  __device__ __forceinline__ uint32_t codes(float s) const {
+    float r, y[8];
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
+    for (int i = 0; i < 4; ++i)
+      asm("{\n\t.reg .b64 x, r, c, d;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 r, {%4, %4};\n\t"
+          "mov.b64 c, {%5, %5};\n\tmov.b64 d, {%6, %6};\n\tfma.rn.f32x2 x, x, r, c;\n\t"
+          "add.rn.f32x2 x, x, d;\n\tmov.b64 {%0, %1}, x;\n\t}"
+          : "=f"(y[2 * i]), "=f"(y[2 * i + 1])
+          : "r"(w[i] << 16), "r"(w[i] & 0xFFFF0000u), "f"(r), "f"(768.f), "f"(-768.f));
+    return pack_codes(y);
   }
   static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float *x) {
     uint32_t w[4];
@@ -51,29 +105,95 @@ struct Eight<__nv_bfloat16> {
     }
     __stcs((uint4 *)p, make_uint4(w[0], w[1], w[2], w[3]));
   }
-  // x / s on the grid of the codes.  With r the rounded reciprocal of the four-bit s,
-  // x r + 768 rounds to whole steps of 2^-14, far above r's error and far below the
-  // distance of an eight-bit x from a midpoint of the codes (at least 2^-10 where
-  // it is not one), so ties are ties and everything else keeps its side.
-  static __device__ __forceinline__ float quotient(float x, float, float r) {
-    return __fadd_rn(__fmaf_rn(x, r, 768.f), -768.f);
-  }
 };
 template <>
 struct Eight<float> {
-  static __device__ __forceinline__ void load(const float *p, float *x) {
-    const float4 a = __ldcs((const float4 *)p), b = __ldcs((const float4 *)p + 1);
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-    x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  float4 a, b;
+  __device__ __forceinline__ void load(const float *p) {
+    a = __ldcs((const float4 *)p);
+    b = __ldcs((const float4 *)p + 1);
+  }
+  __device__ __forceinline__ uint32_t magnitude() const {
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    return m;
+  }
+  static __device__ __forceinline__ uint32_t scale_code(float x) { return pack_scale_code(x); }
+  // As above, but a 24-bit x may lie nearer to a midpoint than a step of 2^-14: where x r + 768
+  // is a multiple of a quarter, as every midpoint is, the entries are divided.
+  __device__ __forceinline__ uint32_t codes(float s) const {
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float r, y[8];
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    uint32_t near = 0xFFFu;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = __fmaf_rn(x[i], r, 768.f);
+      near = min(near, __float_as_uint(f) & 0xFFFu);
+      y[i] = __fadd_rn(f, -768.f);
+    }
+    if (near == 0)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = __fdiv_rn(x[i], s);
+    return pack_codes(y);
   }
   static __device__ __forceinline__ void store(float *p, const float *x) {
     __stcs((float4 *)p, make_float4(x[0], x[1], x[2], x[3]));
     __stcs((float4 *)p + 1, make_float4(x[4], x[5], x[6], x[7]));
   }
-  static __device__ __forceinline__ float quotient(float x, float s, float) {
-    return __fdiv_rn(x, s);
-  }
 };
+
+// Scale codes of n rows' groups, as this thread's eight entries and its neighbour's (lane
+// ^ 1) make them up; rows with a NaN or an infinity anywhere (rowmask: the lanes of a
+// row) get PACK_NAN.
+template <int N>
+__device__ __forceinline__ void scale_codes(const Eight<float> *x, uint32_t rowmask, uint32_t *sc) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    uint32_t m = x[j].magnitude();
+    const bool bad = (__ballot_sync(0xFFFFFFFFu, m >= 0x7F800000u) & rowmask) != 0;
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    sc[j] = bad ? PACK_NAN : pack_scale_code(__uint_as_float(m));
+  }
+}
+// Two bf16 rows at a time: their magnitudes, halves of the sixths and codes in the 16-bit
+// halves of one register each (see pack_scale_code_bf16).
+template <int N>
+__device__ __forceinline__ void scale_codes(const Eight<__nv_bfloat16> *x, uint32_t rowmask,
+                                            uint32_t *sc) {
+  uint32_t m[N / 2], worst = 0, least = 0xFFFFFFFFu;
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) {
+    const uint32_t a = x[2 * j].magnitudes(), b = x[2 * j + 1].magnitudes();
+    m[j] = max_u16x2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+    worst = max_u16x2(worst, m[j]);
+    m[j] = max_u16x2(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 1));
+    least = __vminu2(least, m[j]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) sc[2 * j + h] = 0;
+    const __half2 s = __floats2half2_rn(__uint_as_float(m[j] << 16) * (1.f / 6.f),
+                                        __uint_as_float(m[j] & 0xFFFF0000u) * (1.f / 6.f));
+    const uint32_t u = *(const uint32_t *)&s;
+    const uint32_t c = __vminu2((u + 0x003F003Fu + (u >> 7 & 0x00010001u)) >> 7 & 0x01FF01FFu,
+                                PACK_MAX_CODE * 0x00010001u);
+    sc[2 * j] = c & 0xFFFFu;
+    sc[2 * j + 1] = c >> 16;
+  }
+  // anything not finite, or below 6 * 2^-14 (bf16 bits 0x39C0): rare
+  const bool odd = (worst & 0xFFFFu) >= 0x7F80u || worst >> 16 >= 0x7F80u ||
+                   (least & 0xFFFFu) < 0x39C0u || least >> 16 < 0x39C0u;
+  if (__any_sync(0xFFFFFFFFu, odd)) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint32_t own = x[j].magnitude();
+      const bool bad = (__ballot_sync(0xFFFFFFFFu, own >= 0x7F800000u) & rowmask) != 0;
+      const uint32_t g = j & 1 ? m[j / 2] & 0xFFFF0000u : m[j / 2] << 16;
+      sc[j] = bad ? PACK_NAN : pack_scale_code_bf16(__uint_as_float(g));
+    }
+  }
+}
 
 // Four keys (4 kg ..) x eight entries (8 ch ..) of a block's half in shared memory, as one
 // thread takes them: a word of eight codes per key.
@@ -87,34 +207,37 @@ __device__ __forceinline__ void k_codes_load(const uint8_t *half, int kg, int ch
     c[j + 2] = __byte_perm(a, b, 0x7632);
   }
 }
-template <int DH>
-__device__ __forceinline__ void k_codes_store(uint8_t *half, int kg, int ch, const uint32_t *c) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    *(uint32_t *)(half + pack_k_code(DH, 4 * kg + j, 8 * ch)) = __byte_perm(c[j], c[j + 2], 0x5410);
-    *(uint32_t *)(half + pack_k_code(DH, 4 * kg + j, 8 * ch + 4)) =
-        __byte_perm(c[j], c[j + 2], 0x7632);
-  }
+// V: the nibbles of four keys' words and of eight entries' half-words are each other's
+// transpose (h: entries 0 and 2, 4 and 6, 1 and 3, 5 and 7).
+__device__ __forceinline__ void transpose_out(const uint32_t *c, uint32_t *h) {
+  constexpr uint32_t M = 0x0F0F0F0Fu;
+  const uint32_t a0 = (c[0] & M) | (c[1] << 4 & ~M), a1 = (c[0] >> 4 & M) | (c[1] & ~M);
+  const uint32_t b0 = (c[2] & M) | (c[3] << 4 & ~M), b1 = (c[2] >> 4 & M) | (c[3] & ~M);
+  h[0] = __byte_perm(a0, b0, 0x5140);
+  h[1] = __byte_perm(a0, b0, 0x7362);
+  h[2] = __byte_perm(a1, b1, 0x5140);
+  h[3] = __byte_perm(a1, b1, 0x7362);
+}
+__device__ __forceinline__ void transpose_in(const uint32_t *h, uint32_t *c) {
+  constexpr uint32_t M = 0x0F0F0F0Fu;
+  const uint32_t a0 = __byte_perm(h[0], h[1], 0x6420), b0 = __byte_perm(h[0], h[1], 0x7531);
+  const uint32_t a1 = __byte_perm(h[2], h[3], 0x6420), b1 = __byte_perm(h[2], h[3], 0x7531);
+  c[0] = (a0 & M) | (a1 << 4 & ~M);
+  c[1] = (a0 >> 4 & M) | (a1 & ~M);
+  c[2] = (b0 & M) | (b1 << 4 & ~M);
+  c[3] = (b0 >> 4 & M) | (b1 & ~M);
 }
 __device__ __forceinline__ void v_codes_load(const uint8_t *half, int kg, int ch, uint32_t *c) {
-  c[0] = c[1] = c[2] = c[3] = 0;
+  uint32_t e[8], h[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t h = *(const uint16_t *)(half + pack_v_code(kg, 8 * ch + i));
+  for (int i = 0; i < 8; ++i) e[i] = *(const uint16_t *)(half + pack_v_code(kg, 8 * ch + i));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] |= (h >> (4 * j) & 15u) << (4 * i);
+  for (int i = 0; i < 4; ++i) {
+    const int x = (i & 1) * 4 + (i >> 1);
+    h[i] = e[x] | e[x + 2] << 16;
   }
+  transpose_in(h, c);
 }
-__device__ __forceinline__ void v_codes_store(uint8_t *half, int kg, int ch, const uint32_t *c) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    uint32_t h = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) h |= (c[j] >> (4 * i) & 15u) << (4 * j);
-    *(uint16_t *)(half + pack_v_code(kg, 8 * ch + i)) = (uint16_t)h;
-  }
-}
-
 // Values of eight codes with scale code sc, as halves (exact).
 __device__ __forceinline__ void eight_values(uint32_t c, uint32_t sc, __half2 *v) {
   const uint32_t s2 = sc << 7 | sc << 23;
@@ -132,160 +255,345 @@ __device__ __forceinline__ float unit_of(float a) {
   return __uint_as_float((uint32_t)max(e, 27) << 23);  // 2^-100 and up
 }
 
-// A CTA per (KV head, page, layer): the page's rows are quantised into a copy of the
-// block in shared memory (the present one where the call does not write all of
-// it), the key bounds taken over all rows present, and the block stored whole.
-template <int DH, typename T>
-__global__ void __launch_bounds__(2 * DH)
-    k_packed_write(const PackedView v, const __grid_constant__ PackedRows rows, int len, int l0,
-                   const T *k, const T *val) {
-  constexpr int NT = 2 * DH, CH = DH / 8, HB = pack_half_bytes(DH);
-  __shared__ __align__(16) uint8_t blk[2 * HB];
-  __shared__ int row_of[KVR_PAGE];
-  __shared__ __half2 red[2][NT / 32][DH / 2];
-  __shared__ float amax[DH / 32];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int g = blockIdx.x, l = blockIdx.z;
-  pdl_trigger();
-  pdl_wait();
-  const Segment sg = segment(rows, blockIdx.y);
-  const int present = min(KVR_PAGE, len - sg.page * KVR_PAGE);
-  const bool whole = sg.r1 - sg.r0 == KVR_PAGE;
-  uint8_t *dst = v.block(l0 + l, g, sg.page);
-  if (tid < KVR_PAGE) row_of[tid] = -1;
-  if (!whole)
-    for (int i = tid; i < 2 * HB / 16; i += NT) ((uint4 *)blk)[i] = ((const uint4 *)dst)[i];
-  __syncthreads();
-  for (int i = sg.r0 + tid; i < sg.r1; i += NT) row_of[position(rows, i) % KVR_PAGE] = i;
-  __syncthreads();
-
-  // four keys, eight entries a thread; the CH threads of a row are neighbours
-  const int kg = tid / CH, ch = tid % CH;
-  const uint32_t rowmask = (CH == 16 ? 0xFFFFu : 0xFFu) << (lane & ~(CH - 1));
-  int rr[4];
+// Bounds of the keys of a block, over the finite rows of the slots below `present`, by the
+// first DH / 64 warps of the CTA: warp d4 holds its db's 4 d4 .. + 3, a thread four
+// entries of two keys of each of the four key tiles (w: codes, sc: the keys' scales).
+// What is left is over the eight lanes of a column: each exchange halves what a lane
+// goes on with.  (By all eight warps, a key tile each, the exchanges alone cost as much
+// as all the rest.)
+template <int DH>
+__device__ __forceinline__ void block_bounds(float *amax, const uint32_t (*w)[4],
+                                             const uint32_t (*sc)[2], int present, int8_t *bounds,
+                                             float *unit) {
+  const int lane = threadIdx.x & 31, d4 = threadIdx.x / 32, lg = lane >> 2, lt = lane & 3;
+  __half2 hi[8], lo[8];  // [db of the four][entries 4 lt, 4 lt + 2]
 #pragma unroll
-  for (int j = 0; j < 4; ++j) rr[j] = row_of[4 * kg + j];
-  const bool any = rr[0] >= 0 || rr[1] >= 0 || rr[2] >= 0 || rr[3] >= 0;
-  const bool all = rr[0] >= 0 && rr[1] >= 0 && rr[2] >= 0 && rr[3] >= 0;
-  __half2 hi[4], lo[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 8; ++i) {
     hi[i] = __half2half2(__ushort_as_half(0xFC00));  // -inf
     lo[i] = __half2half2(__ushort_as_half(0x7C00));
   }
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    const T *src = kv ? val : k;
-    uint8_t *half = blk + kv * HB;
-    uint32_t c[4] = {0, 0, 0, 0}, sc[4];
-    float x[4][8];
+  for (int kt = 0; kt < 4; ++kt) {
+    uint32_t v[4][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (rr[j] >= 0) {
-        Eight<T>::load(src + (((size_t)rr[j] * gridDim.z + l) * v.G + g) * DH + 8 * ch, x[j]);
-      } else {
+    for (int b = 0; b < 4; ++b) pack_values(w[kt][b], v[b]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
-      }
-    if (!all) {
-      if (kv)
-        v_codes_load(half, kg, ch, c);
-      else
-        k_codes_load<DH>(half, kg, ch, c);
-    }
+    for (int h = 0; h < 2; ++h) {
+      // all scales of a row marked NaN are
+      if (16 * kt + pack_key_of(lg) + 2 * h >= present || (sc[kt][h] & 0xFF) == PACK_NAN) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      int m = 0;  // largest magnitude's bits: infinities and NaN lie above all others
+      for (int b = 0; b < 4; ++b) {
+        const uint32_t s2 = __byte_perm(sc[kt][h], 0, 0x4040 | b | b << 8) << 7;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, (int)(__float_as_uint(x[j][i]) & 0x7FFFFFFFu));
-      const bool bad = (__ballot_sync(0xFFFFFFFFu, m >= 0x7F800000) & rowmask) != 0;
-      m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-      const int at = kv ? pack_v_scale(DH, 4 * kg + j, ch >> 1)
-                        : pack_k_scale(DH, 4 * kg + j, ch >> 1);
-      if (rr[j] < 0) {
-        sc[j] = half[at];
-        continue;
-      }
-      sc[j] = bad ? PACK_NAN : pack_scale_code(__int_as_float(m));
-      const float s = pack_scale(sc[j]), r = s > 0.f ? __frcp_rn(s) : 0.f;
-      uint32_t w = 0;
-      if (!bad && s > 0.f) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w |= pack_codes(Eight<T>::quotient(x[j][2 * i], s, r),
-                          Eight<T>::quotient(x[j][2 * i + 1], s, r))
-               << (8 * i);
-      }
-      c[j] = w;
-      if (!(ch & 1)) half[at] = (uint8_t)sc[j];
-    }
-    if (any) {
-      if (kv)
-        v_codes_store(half, kg, ch, c);
-      else
-        k_codes_store<DH>(half, kg, ch, c);
-    }
-    if (!kv) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (4 * kg + j >= present || sc[j] == PACK_NAN) continue;
-        __half2 y[4];
-        eight_values(c[j], sc[j], y);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          hi[i] = __hmax2(hi[i], y[i]);
-          lo[i] = __hmin2(lo[i], y[i]);
+        for (int x = 0; x < 2; ++x) {
+          const __half2 y = __hmul2(*(const __half2 *)&v[b][2 * h + x], *(const __half2 *)&s2);
+          hi[2 * b + x] = __hmax2(hi[2 * b + x], y);
+          lo[2 * b + x] = __hmin2(lo[2 * b + x], y);
         }
       }
     }
   }
-  // bounds: over the key groups of the warp, then over the warps
+  // lanes apart by 16, 8, 4: each keeps the half of its entries that its bit of lg names
+#pragma unroll
+  for (int n = 4, o = 16; n; n /= 2, o /= 2) {
+    const bool upper = lane & o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const __half2 sh = upper ? hi[i] : hi[i + n], sl = upper ? lo[i] : lo[i + n];
+      const __half2 kh = upper ? hi[i + n] : hi[i], kl = upper ? lo[i + n] : lo[i];
+      hi[i] = __hmax2(kh, __shfl_xor_sync(0xFFFFFFFFu, sh, o));
+      lo[i] = __hmin2(kl, __shfl_xor_sync(0xFFFFFFFFu, sl, o));
+    }
+  }
+  // lane (lg, lt) holds db 4 d4 + lg / 2, entries 4 lt + 2 (lg & 1) and the next
+  const int at = 16 * (4 * d4 + (lg >> 1)) + 4 * lt + 2 * (lg & 1);
+  float2 h = __half22float2(hi[0]), l = __half22float2(lo[0]);
+  if (h.x < l.x) h = l = make_float2(0.f, 0.f);  // no finite row
+  float a = fmaxf(fmaxf(fabsf(h.x), fabsf(h.y)), fmaxf(fabsf(l.x), fabsf(l.y)));
+#pragma unroll
+  for (int o = 16; o; o /= 2) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+  if (DH > 64) {
+    if (lane == 0) amax[d4] = a;
+    asm volatile("bar.sync 1, %0;" ::"n"(DH / 2) : "memory");
+#pragma unroll
+    for (int i = 0; i < DH / 64; ++i) a = fmaxf(a, amax[i]);
+  }
+  const float u = unit_of(a), r = __frcp_rn(u);  // powers of two: exact
+  auto pair = [](float x, float y) { return (uint16_t)((int)x & 0xFF | (int)y << 8); };
+  *(uint16_t *)(bounds + at) = pair(ceilf(h.x * r), ceilf(h.y * r));
+  *(uint16_t *)(bounds + DH + at) = pair(floorf(l.x * r), floorf(l.y * r));
+  if (threadIdx.x == 0) *unit = u;
+}
+// The same from a K half in shared memory.
+template <int DH>
+__device__ __forceinline__ void block_bounds(float *amax, const uint8_t *kb, int present,
+                                             int8_t *bounds, float *unit) {
+  const int lane = threadIdx.x & 31, d4 = threadIdx.x / 32;
+  uint32_t w[4][4], sc[4][2];
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt) {
+    const uint4 x = *(const uint4 *)(kb + ((kt * (DH / 64) + d4) * 32 + lane) * 16);
+    w[kt][0] = x.x, w[kt][1] = x.y, w[kt][2] = x.z, w[kt][3] = x.w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      sc[kt][h] = *(const uint32_t *)(kb + pack_code_bytes(DH) +
+                                      ((kt * 8 + (lane >> 2)) * 2 + h) * (DH / 16) + 4 * d4);
+  }
+  block_bounds<DH>(amax, w, sc, present, bounds, unit);
+}
+
+// Pages of n consecutive positions from the start of page0 (the last page may end early: the
+// document ends there, and the slots behind stay zero): a CTA per (KV head, page, layer) quantises the
+// page's rows into shared memory (four keys, eight entries of K and of V a thread),
+// takes the bounds from there, and stores the block as it lies there.  Bound by its
+// instructions (14 an entry at first, 233 million for 5000 rows of 32 layers): hence
+// two rows' scales in one register, packed fp32 pairs, and addresses that differ by
+// constants.
+template <int DH, typename T>
+__global__ void __launch_bounds__(2 * DH, sizeof(T) == 2 ? 512 / DH : 256 / DH)
+    k_packed_write_pages(const PackedView v, int page0, int n, int l0, const T *k, const T *val) {
+  constexpr int NT = 2 * DH, CH = DH / 8, HB = pack_half_bytes(DH);
+  __shared__ __align__(16) uint8_t blk[2 * HB];
+  __shared__ float amax[2];
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int g = blockIdx.x, l = blockIdx.z, page = page0 + blockIdx.y;
+  pdl_trigger();
+  pdl_wait();
+  const int kg = tid / CH, ch = tid % CH;  // the CH threads of a row are neighbours
+  const uint32_t rowmask = (CH == 16 ? 0xFFFFu : 0xFFu) << (lane & ~(CH - 1));
+  const size_t row = (size_t)gridDim.z * v.G * DH;
+  const size_t src = ((size_t)(KVR_PAGE * blockIdx.y + 4 * kg) * gridDim.z + l) * v.G * DH +
+                     (size_t)g * DH + 8 * ch;
+  const int present = min(KVR_PAGE, n - KVR_PAGE * (int)blockIdx.y);
+  Eight<T> x[8];  // K's four rows, V's four
+  if (present == KVR_PAGE) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j].load(k + src + j * row);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[4 + j].load(val + src + j * row);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] = x[4 + j] = Eight<T>{};
+      if (4 * kg + j < present) {
+        x[j].load(k + src + j * row);
+        x[4 + j].load(val + src + j * row);
+      }
+    }
+  }
+  uint32_t sc[8], c[8];
+  scale_codes<8>(x, rowmask, sc);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    c[j] = sc[j] == 0 || sc[j] == PACK_NAN ? 0 : x[j].codes(pack_scale(sc[j]));
+  // K: words of keys j and j + 2 lie 64 bytes on for the next j, 16 for four more entries
+  uint8_t *kb = blk, *vb = blk + HB;
+  uint32_t *kw = (uint32_t *)(kb + pack_k_code(DH, 4 * kg, 8 * ch));
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    kw[16 * j] = __byte_perm(c[j], c[j + 2], 0x5410);
+    kw[16 * j + 4] = __byte_perm(c[j], c[j + 2], 0x7632);
+  }
+  // V: entry i's half-word lies 64 (i ^ db / 4) bytes on
+  uint32_t h[4];
+  transpose_out(c + 4, h);
+  const int flip = ch >> 3;
+  uint8_t *v0 = vb + pack_v_code(kg, 8 * ch) - 64 * flip;  // of i = 0 where db < 4
+  uint16_t *ve = (uint16_t *)(v0 + 64 * flip), *vo = (uint16_t *)(v0 - 64 * flip);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    const int e = (i & 1) * 4 + (i >> 1);  // entries e and e + 2: both even or both odd
+    uint16_t *at = (e & 1) ? vo : ve;
+    at[32 * e] = (uint16_t)h[i];
+    at[32 * (e + 2)] = (uint16_t)(h[i] >> 16);
+  }
+  if (!(ch & 1)) {
+    uint8_t *ks = kb + pack_k_scale(DH, 4 * kg, ch >> 1);
+    ks[0] = (uint8_t)sc[0];  // keys 0 and 2 of the four, 1 and 3
+    ks[DH / 16] = (uint8_t)sc[2];
+    ks[2 * (DH / 16)] = (uint8_t)sc[1];
+    ks[3 * (DH / 16)] = (uint8_t)sc[3];
+    *(uint32_t *)(vb + pack_v_scale(DH, 4 * kg, ch >> 1)) =
+        sc[4] | sc[5] << 8 | sc[6] << 16 | sc[7] << 24;
+  }
+  __syncthreads();
+  uint4 *dst = (uint4 *)v.block(l0 + l, g, page);
+  for (int i = tid; i < 2 * HB / 16; i += NT) dst[i] = ((const uint4 *)blk)[i];
+  if (tid >= DH / 2) return;
+  const size_t at = v.index(l0 + l, g, page);
+  block_bounds<DH>(amax, kb, present, v.bounds + at * 2 * DH, v.unit + at);
+}
+
+// Pages that a call writes in part: a CTA per (KV head, page, layer).  The new rows are
+// quantised, K and V side by side in a warp, into shared memory, while the block's K
+// codes are on their way to registers and so are the V codes of the first groups of four
+// keys that change; words with a new key are patched and stored, and the bounds taken
+// over all rows present.  NT: DH / 2 threads for a few rows (the bounds' warps alone,
+// whose registers then hold all they need; 40 rows of 40 pages, 112 CTAs each: 28.6 us
+// by 2 DH threads), 2 DH for many.  which: the segments of a run that are not whole
+// pages (a list's are blockIdx.y).
+constexpr int PATCH_FEW = 4;
+template <int DH, typename T, class Rows, int NT>
+__global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
+    k_packed_patch(const PackedView v, const __grid_constant__ Rows rows, int2 which, int len,
+                   int l0, const T *k, const T *val) {
+  constexpr int CH = DH / 8, DB = DH / 16, DQ = DH / 64, HB = pack_half_bytes(DH),
+                CB = pack_code_bytes(DH), WARPS = NT / 32, KPT = 2 * DH / NT;  // 16 bytes of K a thread
+  constexpr bool FEW = KPT == 4;
+  constexpr int ROWS = FEW ? PATCH_FEW : KVR_PAGE;  // rows in shared memory
+  constexpr int VPT = NT < DH ? DH / NT : 1;        // V entries a thread, VG groups at a time
+  constexpr int VG = NT < DH ? 1 : NT / DH;
+  __shared__ float amax[2];
+  __shared__ __align__(16) uint32_t code[ROWS][2][CH];
+  __shared__ __align__(8) uint8_t scale[ROWS][2][DB];
+  __shared__ uint8_t row_at[KVR_PAGE];  // of a slot that is written
+  __shared__ __align__(16) uint8_t kbuf[FEW ? 16 : HB];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lg = lane >> 2, lt = lane & 3;
+  const int g = blockIdx.x, l = blockIdx.z;
+  pdl_trigger();
+  pdl_wait();
+  const Segment sg = segment(rows, rows.first < 0 ? blockIdx.y : blockIdx.y ? which.y : which.x);
+  const int present = min(KVR_PAGE, len - sg.page * KVR_PAGE), count = sg.r1 - sg.r0;
+  auto slot_of = [&](int i) {
+    return (rows.first >= 0 ? rows.first + sg.r0 + i : position(rows, sg.r0 + i)) % KVR_PAGE;
+  };
+  uint8_t *kb = v.block(l0 + l, g, sg.page), *vb = kb + HB;
+  // K codes: 16 bytes of key tile kt_of(i), db's 4 d4 .. of this lane
+  const int d4 = warp % DQ;
+  auto kt_of = [&](int i) { return FEW ? i : warp / DQ; };
+  uint32_t w[KPT][4], sc[KPT][2];
 #pragma unroll
-    for (int o = CH; o < 32; o *= 2) {
-      hi[i] = __hmax2(hi[i], __shfl_xor_sync(0xFFFFFFFFu, hi[i], o));
-      lo[i] = __hmin2(lo[i], __shfl_xor_sync(0xFFFFFFFFu, lo[i], o));
-    }
-    if (lane < CH) {
-      red[0][warp][4 * lane + i] = hi[i];
-      red[1][warp][4 * lane + i] = lo[i];
+  for (int i = 0; i < KPT; ++i) {
+    const uint4 x = *(const uint4 *)(kb + ((kt_of(i) * DQ + d4) * 32 + lane) * 16);
+    w[i][0] = x.x, w[i][1] = x.y, w[i][2] = x.z, w[i][3] = x.w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      sc[i][h] = *(const uint32_t *)(kb + CB + ((kt_of(i) * 8 + lg) * 2 + h) * DB + 4 * d4);
+  }
+  // the slots that are written
+  uint32_t mlo = 0, mhi = 0;
+  for (int i = lane; i < count; i += 32) {
+    const int s = slot_of(i);
+    (s < 32 ? mlo : mhi) |= 1u << (s & 31);
+    if (warp == 0) row_at[s] = (uint8_t)i;
+  }
+  const unsigned long long mask = __reduce_or_sync(0xFFFFFFFFu, mlo) |
+                                  (unsigned long long)__reduce_or_sync(0xFFFFFFFFu, mhi) << 32;
+  // V codes of a thread's entries, in every VG-th of the groups that change
+  const int e0 = tid % DH;
+  auto next_group = [](unsigned long long &m) {  // the first group of four slots in m, and past it
+    if (!m) return -1;
+    const int kg = (__ffsll((long long)m) - 1) / 4;
+    m &= ~(15ull << (4 * kg));
+    return kg;
+  };
+  unsigned long long mine = mask;
+  if (VG > 1 && tid >= DH) next_group(mine);
+  int kg = next_group(mine);
+  uint32_t old[VPT];
+  auto fetch_old = [&]() {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      if (kg >= 0) old[i] = *(const uint16_t *)(vb + pack_v_code(kg, e0 + i * NT));
+  };
+  fetch_old();
+  // the new rows, up to PRE of a warp's in flight
+  {
+    const int sub = lane / CH, ch = lane % CH;  // rows' halves side by side: K, V (twice for 64)
+    const uint32_t rowmask = (CH == 16 ? 0xFFFFu : 0xFFu) << (lane & ~(CH - 1));
+    constexpr int RPW = 32 / (2 * CH), PRE = FEW ? 2 : 4;  // rows of a warp at a time
+    for (int i0 = warp * RPW; i0 < count; i0 += WARPS * RPW * PRE) {
+      Eight<T> x[PRE];
+#pragma unroll
+      for (int j = 0; j < PRE; ++j) {
+        const int i = i0 + j * WARPS * RPW + sub / 2;
+        x[j] = Eight<T>{};
+        if (i < count)
+          x[j].load((sub & 1 ? val : k) + (((size_t)(sg.r0 + i) * gridDim.z + l) * v.G + g) * DH +
+                    8 * ch);
+      }
+#pragma unroll
+      for (int j = 0; j < PRE; ++j) {
+        const int i = i0 + j * WARPS * RPW + sub / 2;
+        if (i0 + j * WARPS * RPW >= count) break;
+        uint32_t m = x[j].magnitude();
+        const bool bad = (__ballot_sync(0xFFFFFFFFu, m >= 0x7F800000u) & rowmask) != 0;
+        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+        if (i < count) {
+          const uint32_t s = bad ? PACK_NAN : Eight<T>::scale_code(__uint_as_float(m));
+          code[i][sub & 1][ch] = bad || s == 0 ? 0 : x[j].codes(pack_scale(s));
+          if (!(ch & 1)) scale[i][sub & 1][ch >> 1] = (uint8_t)s;
+        }
+        __syncwarp();
+      }
     }
   }
   __syncthreads();
-  float h = -INFINITY, b = INFINITY;
-  if (tid < DH) {
+  // K: the half-words of this thread's keys
 #pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-      h = fmaxf(h, __half2float(((const __half *)red[0][w])[tid]));
-      b = fminf(b, __half2float(((const __half *)red[1][w])[tid]));
+  for (int i = 0; i < KPT; ++i) {
+    bool changed = false;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int key = 16 * kt_of(i) + pack_key_of(lg) + 2 * h;
+      if (mask >> key & 1) {
+        changed = true;
+        const int r = row_at[key];
+        const uint16_t *c = (const uint16_t *)code[r][0] + 16 * d4 + lt;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) w[i][b] = __byte_perm(w[i][b], c[4 * b], h ? 0x5410 : 0x3254);
+        sc[i][h] = *(const uint32_t *)&scale[r][0][4 * d4];
+        if (lt == 0)
+          *(uint32_t *)(kb + CB + ((kt_of(i) * 8 + lg) * 2 + h) * DB + 4 * d4) = sc[i][h];
+      }
     }
-    if (h < b) h = b = 0.f;  // no finite row
-    float a = fmaxf(fabsf(h), fabsf(b));
+    const int off = ((kt_of(i) * DQ + d4) * 32 + lane) * 16;
+    if (changed) *(uint4 *)(kb + off) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+    if constexpr (!FEW) {
+      *(uint4 *)(kbuf + off) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+      if (lt == 0)
 #pragma unroll
-    for (int o = 16; o; o /= 2) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
-    if (lane == 0) amax[warp] = a;
+        for (int h = 0; h < 2; ++h)
+          *(uint32_t *)(kbuf + CB + ((kt_of(i) * 8 + lg) * 2 + h) * DB + 4 * d4) = sc[i][h];
+    }
   }
-  for (int i = tid; i < 2 * HB / 16; i += NT) ((uint4 *)dst)[i] = ((const uint4 *)blk)[i];
-  __syncthreads();
-  if (tid < DH) {
-    float a = amax[0];
+  // V: the half-words of a group
+  while (kg >= 0) {
 #pragma unroll
-    for (int w = 1; w < DH / 32; ++w) a = fmaxf(a, amax[w]);
-    const float u = unit_of(a), r = __frcp_rn(u);  // powers of two: exact
-    const size_t at = v.index(l0 + l, g, sg.page);
-    v.bounds[at * 2 * DH + tid] = (int8_t)ceilf(h * r);
-    v.bounds[at * 2 * DH + DH + tid] = (int8_t)floorf(b * r);
-    if (tid == 0) v.unit[at] = u;
+    for (int j = 0; j < 4; ++j)
+      if (mask >> (4 * kg + j) & 1) {
+        const int r = row_at[4 * kg + j];
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+          const int e = e0 + i * NT;
+          const uint32_t n = code[r][1][e >> 3] >> (4 * (e & 7)) & 15u;
+          old[i] = (old[i] & ~(15u << (4 * j))) | n << (4 * j);
+        }
+      }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      *(uint16_t *)(vb + pack_v_code(kg, e0 + i * NT)) = (uint16_t)old[i];
+    if (VG > 1) next_group(mine);  // the other half's
+    kg = next_group(mine);
+    fetch_old();
+  }
+  for (int i = tid; i < count * DB; i += NT)
+    vb[pack_v_scale(DH, slot_of(i / DB), i % DB)] = scale[i / DB][1][i % DB];
+  const size_t at = v.index(l0 + l, g, sg.page);
+  if constexpr (FEW) {
+    block_bounds<DH>(amax, w, sc, present, v.bounds + at * 2 * DH, v.unit + at);
+  } else {
+    __syncthreads();
+    if (tid < DH / 2)
+      block_bounds<DH>(amax, kbuf, present, v.bounds + at * 2 * DH, v.unit + at);
   }
 }
 
 // A CTA per (KV head, page, layer): the block into shared memory, the rows asked for out
 // of it.
-template <int DH, typename T>
+template <int DH, typename T, class Rows>
 __global__ void __launch_bounds__(2 * DH)
-    k_packed_read(const PackedView v, const __grid_constant__ PackedRows rows, int l0, T *k,
-                  T *val) {
+    k_packed_read(const PackedView v, const __grid_constant__ Rows rows, int l0, T *k, T *val) {
   constexpr int NT = 2 * DH, CH = DH / 8, HB = pack_half_bytes(DH);
   __shared__ __align__(16) uint8_t blk[2 * HB];
   __shared__ int row_of[KVR_PAGE];
@@ -294,15 +602,11 @@ __global__ void __launch_bounds__(2 * DH)
   pdl_wait();
   const Segment sg = segment(rows, blockIdx.y);
   const uint8_t *src = v.block(l0 + l, g, sg.page);
-  if (tid < KVR_PAGE) row_of[tid] = -1;
   for (int i = tid; i < 2 * HB / 16; i += NT) ((uint4 *)blk)[i] = ((const uint4 *)src)[i];
-  __syncthreads();
-  for (int i = sg.r0 + tid; i < sg.r1; i += NT) row_of[position(rows, i) % KVR_PAGE] = i;
-  __syncthreads();
   const int kg = tid / CH, ch = tid % CH;
   int rr[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) rr[j] = row_of[4 * kg + j];
+  rows_of_slots(rows, sg, row_of, kg, rr);
+  __syncthreads();
   if (rr[0] < 0 && rr[1] < 0 && rr[2] < 0 && rr[3] < 0) return;
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
@@ -527,34 +831,84 @@ PerDevice<size_t> sel_smem[4];
 
 }  // namespace
 
-void launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows, int len, int l0,
-                         int nl, const void *k, const void *val, cudaStream_t s) {
-  const dim3 grid(v.G, rows.n_seg, nl);
-  auto run = [&](auto kernel, auto *kk, auto *vv) {
-    launch_pdl(kernel, grid, dim3(2 * v.dh), 0, s, v, rows, len, l0, kk, vv);
-  };
-  if (dtype == KVR_DTYPE_BF16) {
-    using T = __nv_bfloat16;
-    run(v.dh == 128 ? k_packed_write<128, T> : k_packed_write<64, T>, (const T *)k, (const T *)val);
-  } else {
-    run(v.dh == 128 ? k_packed_write<128, float> : k_packed_write<64, float>, (const float *)k,
-        (const float *)val);
+namespace {
+// Pages that a run writes whole by k_packed_write_pages, all others by k_packed_patch.
+template <int DH, typename T, class Rows>
+int write_rows(const PackedView &v, const Rows &rows, int len, int l0, int nl, const void *k,
+               const void *val, cudaStream_t s) {
+  int2 part{0, 0};
+  int parts = rows.n_seg, launches = 0, most = rows.most;
+  if (rows.first >= 0) {
+    // whole pages [p0, p1), the last of which may end where the document does
+    const int end = rows.first + rows.n, p0 = (rows.first + KVR_PAGE - 1) / KVR_PAGE,
+              p1 = end == len ? (end + KVR_PAGE - 1) / KVR_PAGE : end / KVR_PAGE;
+    const int head = rows.first % KVR_PAGE ? std::min(rows.n, p0 * KVR_PAGE - rows.first) : 0;
+    const int tail = p1 * KVR_PAGE >= end ? 0 : end - std::max(p1 * KVR_PAGE, rows.first + head);
+    parts = most = 0;
+    if (head) parts = 1, most = head;
+    if (tail) (parts ? part.y : part.x) = rows.n_seg - 1, ++parts, most = std::max(most, tail);
+    if (p1 > p0) {
+      const size_t skip = (size_t)(p0 * KVR_PAGE - rows.first) * nl * v.G * DH;
+      launch_pdl(k_packed_write_pages<DH, T>, dim3(v.G, p1 - p0, nl), dim3(2 * DH), 0, s, v, p0,
+                 end - p0 * KVR_PAGE, l0, (const T *)k + skip, (const T *)val + skip);
+      ++launches;
+    }
   }
+  if (parts) {
+    auto patch = [&](auto kernel, int threads) {
+      launch_pdl(kernel, dim3(v.G, parts, nl), dim3(threads), 0, s, v, rows, part, len, l0,
+                 (const T *)k, (const T *)val);
+    };
+    if (most <= PATCH_FEW)
+      patch(k_packed_patch<DH, T, Rows, DH / 2>, DH / 2);
+    else
+      patch(k_packed_patch<DH, T, Rows, 2 * DH>, 2 * DH);
+    ++launches;
+  }
+  return launches;
+}
+template <int DH, typename T, class Rows>
+void read_rows(const PackedView &v, const Rows &rows, int l0, int nl, void *k, void *val,
+               cudaStream_t s) {
+  launch_pdl(k_packed_read<DH, T, Rows>, dim3(v.G, rows.n_seg, nl), dim3(2 * DH), 0, s, v, rows, l0,
+             (T *)k, (T *)val);
+}
+// f with the head size, the type and the kind of rows as template arguments.
+template <class F>
+void by_kind(int dh, int dtype, const PackedRows &rows, F f) {
+  auto typed = [&](auto d, auto t) {
+    if (rows.inlined)
+      f(d, t, rows.list);
+    else
+      f(d, t, (const PackedRun &)rows.list);
+  };
+  auto sized = [&](auto d) {
+    if (dtype == KVR_DTYPE_BF16)
+      typed(d, __nv_bfloat16{});
+    else
+      typed(d, float{});
+  };
+  if (dh == 128)
+    sized(std::integral_constant<int, 128>{});
+  else
+    sized(std::integral_constant<int, 64>{});
+}
+}  // namespace
+
+int launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows, int len, int l0,
+                        int nl, const void *k, const void *val, cudaStream_t s) {
+  int launches = 0;
+  by_kind(v.dh, dtype, rows, [&](auto d, auto t, const auto &r) {
+    launches = write_rows<decltype(d)::value, decltype(t)>(v, r, len, l0, nl, k, val, s);
+  });
+  return launches;
 }
 
 void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, int l0, int nl,
                         void *k, void *val, cudaStream_t s) {
-  const dim3 grid(v.G, rows.n_seg, nl);
-  auto run = [&](auto kernel, auto *kk, auto *vv) {
-    launch_pdl(kernel, grid, dim3(2 * v.dh), 0, s, v, rows, l0, kk, vv);
-  };
-  if (dtype == KVR_DTYPE_BF16) {
-    using T = __nv_bfloat16;
-    run(v.dh == 128 ? k_packed_read<128, T> : k_packed_read<64, T>, (T *)k, (T *)val);
-  } else {
-    run(v.dh == 128 ? k_packed_read<128, float> : k_packed_read<64, float>, (float *)k,
-        (float *)val);
-  }
+  by_kind(v.dh, dtype, rows, [&](auto d, auto t, const auto &r) {
+    read_rows<decltype(d)::value, decltype(t)>(v, r, l0, nl, k, val, s);
+  });
 }
 
 void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, const void *q,

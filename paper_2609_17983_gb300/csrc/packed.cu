@@ -58,25 +58,31 @@ kvr_status check_device_ptr(const kvr_model *m, const void *p, const char *name)
 
 // Positions of a call (ascending) in segments of a page each; many scattered ones go to
 // the model's readback scratch.
-kvr_status rows_of(kvr_model *m, const int32_t *pos, int n, PackedRows &r) {
+kvr_status rows_of(kvr_model *m, const int32_t *pos, int n, PackedRows &rows) {
+  PackedList &r = rows.list;
   r.n = n;
   if (pos[n - 1] - pos[0] == n - 1) {
     r.first = pos[0];
     r.n_seg = pos[n - 1] / KVR_PAGE - pos[0] / KVR_PAGE + 1;
     return KVR_OK;
   }
-  std::vector<int32_t> seg;
-  for (int i = 0; i < n; ++i)
-    if (!i || pos[i] / KVR_PAGE != pos[i - 1] / KVR_PAGE) seg.push_back(i);
-  r.n_seg = (int)seg.size();
-  seg.push_back(n);
-  if (n <= PACK_INLINE_POS) {
-    for (size_t i = 0; i < seg.size(); ++i) r.seg[i] = (uint16_t)seg[i];
+  for (int i = 0, at = 0; i < n; ++i) {
+    if (pos[i] / KVR_PAGE != pos[at] / KVR_PAGE) at = i;
+    r.most = std::max(r.most, i - at + 1);
+  }
+  rows.inlined = n <= PACK_INLINE_POS;
+  if (rows.inlined) {
+    for (int i = 0; i < n; ++i)
+      if (!i || pos[i] / KVR_PAGE != pos[i - 1] / KVR_PAGE) r.seg[r.n_seg++] = (uint16_t)i;
+    r.seg[r.n_seg] = (uint16_t)n;
     memcpy(r.pos, pos, n * sizeof(int32_t));
     return KVR_OK;
   }
   std::vector<int32_t> all(pos, pos + n);
-  all.insert(all.end(), seg.begin(), seg.end());
+  for (int i = 0; i < n; ++i)
+    if (!i || pos[i] / KVR_PAGE != pos[i - 1] / KVR_PAGE) all.push_back(i);
+  r.n_seg = (int)all.size() - n;
+  all.push_back(n);
   KVR_TRY(grow_device(m, m->read_scratch, m->read_scratch_bytes, all.size() * 4,
                       "readback scratch"));
   KVR_TRY(upload_words(m, m->read_scratch, all.data(), all.size()));
@@ -394,8 +400,8 @@ kvr_status kvr_packed_write(kvr_packed *c, const int32_t *positions, int32_t n_p
   PackedRows rows;
   KVR_TRY(rows_of(m, positions, n_pos, rows));
   const int len = std::max(c->n, positions[n_pos - 1] + 1);
-  launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->stream);
-  const kvr_status st = launched(m, 1, "packed write");
+  const int n = launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->stream);
+  const kvr_status st = launched(m, n, "packed write");
   if (st)
     c->poisoned = true;
   else

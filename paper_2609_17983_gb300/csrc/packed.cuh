@@ -95,24 +95,36 @@ __device__ __forceinline__ void pack_values(uint32_t w, uint32_t *v) {
       : "r"(w));
 }
 
-// Codes of a (low nibble) and b.
-__device__ __forceinline__ uint32_t pack_codes(float a, float b) {
+// The codes of eight entries over their scale, low nibble first.
+__device__ __forceinline__ uint32_t pack_codes(const float *y) {
   uint32_t r;
-  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %2, %1;\n\tcvt.u32.u8 %0, c;\n\t}"
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+      "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
       : "=r"(r)
-      : "f"(a), "f"(b));
+      : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
   return r;
 }
 
 // Scale of a group whose largest magnitude is a (finite), as its code.  The rounding to
-// three mantissa bits is a float's own: above 2^-14 of the mantissa's bits, below in
-// whole steps of 2^-17.
+// three mantissa bits is done on the float's own bits, below 2^-14 in whole steps of
+// 2^-17.
 __device__ __forceinline__ uint32_t pack_scale_code(float a) {
   const float s = fminf(__fdiv_rn(a, 6.f), PACK_MAX_SCALE);
   if (s < 6.103515625e-05f) return (uint32_t)__float2int_rn(s * 131072.f);  // 2^-14, 2^17
   uint32_t u = __float_as_uint(s);
   u = (u + 0x7FFFFu + ((u >> 20) & 1u)) >> 20;  // exponent and three mantissa bits
   return u - ((127 - 15) << 3);
+}
+// The same for a bf16 a.  a / 6 of an eight-bit a is a midpoint of the scales or at least
+// 2^-8 of itself away from one, so rounded to a half (2^-11) the product with the
+// rounded 1 / 6 is on a midpoint exactly where it should be; halves below 2^-14 are too
+// coarse for that.
+__device__ __forceinline__ uint32_t pack_scale_code_bf16(float a) {
+  if (a < 6.f * 6.103515625e-05f) return pack_scale_code(a);
+  const uint32_t h = __half_as_ushort(__float2half_rn(a * (1.f / 6.f)));
+  return min((h + 0x3Fu + ((h >> 7) & 1u)) >> 7, (uint32_t)PACK_MAX_CODE);
 }
 __device__ __forceinline__ float pack_scale(uint32_t code) {
   return __half2float(__ushort_as_half((unsigned short)(code << 7)));
@@ -129,19 +141,27 @@ __device__ __forceinline__ int pack_q_exponent(float a) {
 
 // ---- kernels (k_packed.cu, k_packed_attn.cu) ----
 
-// Positions of a call in segments of one page each.  A run of consecutive positions
-// needs no table; a few come with the launch, more lie in device memory.
+// Positions of a call in segments of one page each: a run of consecutive positions, or
+// a list, which comes with the launch when it is short and else lies in device memory.
 constexpr int PACK_INLINE_POS = 512;
-struct PackedRows {
-  int n = 0, n_seg = 0;
+struct PackedRun {
+  int n = 0, n_seg = 0, most = 0;  // most: rows of a list's fullest segment
   int first = -1;                  // >= 0: positions first .. first + n - 1
-  const int32_t *pos_d = nullptr;  // device [n], then segment starts [n_seg + 1]
+  const int32_t *pos_d = nullptr;  // else device [n], then segment starts [n_seg + 1]
+};
+struct PackedList : PackedRun {
   uint16_t seg[PACK_INLINE_POS + 1];
   int32_t pos[PACK_INLINE_POS];
 };
+// Short lists are the only ones that need more than the run's few bytes of arguments.
+struct PackedRows {
+  PackedList list;
+  bool inlined = false;
+};
 // k, v: [n][nl][G][dh] in the model dtype; len: the document's length after the write.
-void launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows, int len, int l0,
-                         int nl, const void *k, const void *val, cudaStream_t s);
+// Returns the kernels launched.
+int launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows, int len, int l0,
+                        int nl, const void *k, const void *val, cudaStream_t s);
 void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, int l0, int nl,
                         void *k, void *val, cudaStream_t s);
 
