@@ -281,12 +281,15 @@ __device__ __forceinline__ void block_bounds(float *amax, const uint32_t (*w)[4]
     for (int h = 0; h < 2; ++h) {
       // all scales of a row marked NaN are
       if (16 * kt + pack_key_of(lg) + 2 * h >= present || (sc[kt][h] & 0xFF) == PACK_NAN) continue;
+      const uint32_t s01 = __byte_perm(sc[kt][h], 0, 0x4140) << 7,
+                     s23 = __byte_perm(sc[kt][h], 0, 0x4342) << 7;
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const uint32_t s2 = __byte_perm(sc[kt][h], 0, 0x4040 | b | b << 8) << 7;
+        const __half2 two = *(const __half2 *)(b < 2 ? &s01 : &s23),
+                      s2 = b & 1 ? __high2half2(two) : __low2half2(two);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const __half2 y = __hmul2(*(const __half2 *)&v[b][2 * h + x], *(const __half2 *)&s2);
+          const __half2 y = __hmul2(*(const __half2 *)&v[b][2 * h + x], s2);
           hi[2 * b + x] = __hmax2(hi[2 * b + x], y);
           lo[2 * b + x] = __hmin2(lo[2 * b + x], y);
         }
@@ -441,8 +444,7 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
                 CB = pack_code_bytes(DH), WARPS = NT / 32, KPT = 2 * DH / NT;  // 16 bytes of K a thread
   constexpr bool FEW = KPT == 4;
   constexpr int ROWS = FEW ? PATCH_FEW : KVR_PAGE;  // rows in shared memory
-  constexpr int VPT = NT < DH ? DH / NT : 1;        // V entries a thread, VG groups at a time
-  constexpr int VG = NT < DH ? 1 : NT / DH;
+  constexpr int VG = NT / (DH / 2);  // groups of V at a time, a word (entries i, i + 8) a thread
   __shared__ float amax[2];
   __shared__ __align__(16) uint32_t code[ROWS][2][CH];
   __shared__ __align__(8) uint8_t scale[ROWS][2][DB];
@@ -466,9 +468,16 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
   for (int i = 0; i < KPT; ++i) {
     const uint4 x = *(const uint4 *)(kb + ((kt_of(i) * DQ + d4) * 32 + lane) * 16);
     w[i][0] = x.x, w[i][1] = x.y, w[i][2] = x.z, w[i][3] = x.w;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      sc[i][h] = *(const uint32_t *)(kb + CB + ((kt_of(i) * 8 + lg) * 2 + h) * DB + 4 * d4);
+    const uint8_t *ks = kb + CB + (kt_of(i) * 8 + lg) * 2 * DB;  // of both keys
+    if constexpr (DQ == 2) {
+      const uint4 y = *(const uint4 *)ks;
+      sc[i][0] = d4 ? y.y : y.x;
+      sc[i][1] = d4 ? y.w : y.z;
+    } else {
+      const uint2 y = *(const uint2 *)ks;
+      sc[i][0] = y.x;
+      sc[i][1] = y.y;
+    }
   }
   // the slots that are written
   uint32_t mlo = 0, mhi = 0;
@@ -479,8 +488,8 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
   }
   const unsigned long long mask = __reduce_or_sync(0xFFFFFFFFu, mlo) |
                                   (unsigned long long)__reduce_or_sync(0xFFFFFFFFu, mhi) << 32;
-  // V codes of a thread's entries, in every VG-th of the groups that change
-  const int e0 = tid % DH;
+  // V: a thread's word of every VG-th of the groups of four keys that change
+  const int vdb = tid % (DH / 2) >> 3, vi = tid & 7;
   auto next_group = [](unsigned long long &m) {  // the first group of four slots in m, and past it
     if (!m) return -1;
     const int kg = (__ffsll((long long)m) - 1) / 4;
@@ -488,15 +497,10 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
     return kg;
   };
   unsigned long long mine = mask;
-  if (VG > 1 && tid >= DH) next_group(mine);
+  for (int i = 0; i < tid / (DH / 2); ++i) next_group(mine);
   int kg = next_group(mine);
-  uint32_t old[VPT];
-  auto fetch_old = [&]() {
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-      if (kg >= 0) old[i] = *(const uint16_t *)(vb + pack_v_code(kg, e0 + i * NT));
-  };
-  fetch_old();
+  auto v_word = [&]() { return (uint32_t *)(vb + pack_v_code(kg, 16 * vdb + vi)); };
+  uint32_t old = kg >= 0 ? *v_word() : 0;
   // the new rows, up to PRE of a warp's in flight
   {
     const int sub = lane / CH, ch = lane % CH;  // rows' halves side by side: K, V (twice for 64)
@@ -557,25 +561,19 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
           *(uint32_t *)(kbuf + CB + ((kt_of(i) * 8 + lg) * 2 + h) * DB + 4 * d4) = sc[i][h];
     }
   }
-  // V: the half-words of a group
+  // V: the words of a group
   while (kg >= 0) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (mask >> (4 * kg + j) & 1) {
-        const int r = row_at[4 * kg + j];
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-          const int e = e0 + i * NT;
-          const uint32_t n = code[r][1][e >> 3] >> (4 * (e & 7)) & 15u;
-          old[i] = (old[i] & ~(15u << (4 * j))) | n << (4 * j);
-        }
+        const uint32_t *c = code[row_at[4 * kg + j]][1] + 2 * vdb;
+        const uint32_t n = (c[0] >> (4 * vi) & 15u) | (c[1] >> (4 * vi) & 15u) << 16;
+        old = (old & ~(0x000F000Fu << (4 * j))) | n << (4 * j);
       }
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-      *(uint16_t *)(vb + pack_v_code(kg, e0 + i * NT)) = (uint16_t)old[i];
-    if (VG > 1) next_group(mine);  // the other half's
+    *v_word() = old;
+    for (int i = 1; i < VG; ++i) next_group(mine);  // the others'
     kg = next_group(mine);
-    fetch_old();
+    if (kg >= 0) old = *v_word();
   }
   for (int i = tid; i < count * DB; i += NT)
     vb[pack_v_scale(DH, slot_of(i / DB), i % DB)] = scale[i / DB][1][i % DB];

@@ -314,14 +314,14 @@ def kvr_packed_len(packed) -> int:
 def kvr_packed_write(packed, positions, layer_begin: int, layer_end: int, k_dev_ptr: int,
                      v_dev_ptr: int):
     ps = _i32(positions)
-    _check(_lib.kvr_packed_write(packed, _ptr(ps), ps.size, layer_begin, layer_end, k_dev_ptr,
+    _check(_lib.kvr_packed_write(packed, ps.tobytes(), ps.size, layer_begin, layer_end, k_dev_ptr,
                                  v_dev_ptr))
 
 
 def kvr_packed_read(packed, positions, layer_begin: int, layer_end: int, k_dev_ptr: int,
                     v_dev_ptr: int):
     ps = _i32(positions)
-    _check(_lib.kvr_packed_read(packed, _ptr(ps), ps.size, layer_begin, layer_end, k_dev_ptr,
+    _check(_lib.kvr_packed_read(packed, ps.tobytes(), ps.size, layer_begin, layer_end, k_dev_ptr,
                                 v_dev_ptr))
 
 
@@ -654,9 +654,14 @@ class Cache:
                                   c["head_dim"], dt, k_out, v_out)
 
 
-def _device(t, name: str, dtype: str, count: int) -> int:
+def _torch_dtype(cfg: dict):
+    import torch
+    return torch.bfloat16 if cfg["dtype"] == "bf16" else torch.float32
+
+
+def _device(t, name: str, dtype, count: int) -> int:
     """Address of a contiguous CUDA tensor of `count` entries."""
-    if not t.is_cuda or str(t.dtype) != dtype or t.numel() != count or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of {count} entries, "
                          f"not {t.dtype}{list(t.shape)} on {t.device}")
     return t.data_ptr()
@@ -671,7 +676,7 @@ class Packed:
         self.h = handle
         c = model.cfg
         self._row = c["n_kv_heads"] * c["head_dim"]
-        self._dtype = "torch.bfloat16" if c["dtype"] == "bf16" else "torch.float32"
+        self._dtype = _torch_dtype(c)
         model._caches.add(self)
 
     def close(self):
@@ -722,7 +727,9 @@ class Rows:
         self._row = c["n_heads"] * c["head_dim"]
         self._heads = (c["n_heads"], c["head_dim"])
         self._lists = self.n * c["n_kv_heads"]
-        self._dtype = "torch.bfloat16" if c["dtype"] == "bf16" else "torch.float32"
+        self._dtype = _torch_dtype(c)
+        import torch
+        self._int = torch.int32
         self.h = kvr_rows_create(model.h, [(d.h, p) for d, p in docs])
         model._caches.add(self)
 
@@ -747,7 +754,7 @@ class Rows:
         if q.is_contiguous() or q.dim() != 3:
             return _device(q, "q", self._dtype, self.n * self._row), self._row
         H, dh = self._heads
-        if (not q.is_cuda or str(q.dtype) != self._dtype or tuple(q.shape) != (self.n, H, dh) or
+        if (not q.is_cuda or q.dtype is not self._dtype or tuple(q.shape) != (self.n, H, dh) or
                 q.stride(2) != 1 or q.stride(1) != dh):
             raise ValueError(f"q must be {self._dtype} [{self.n}, {H}, {dh}], heads contiguous")
         return q.data_ptr(), q.stride(0)
@@ -762,7 +769,7 @@ class Rows:
             return
         nb = blocks.shape[-1]
         kvr_packed_attention_blocks(self.h, layer, qp, ldq,
-                                    _device(blocks, "blocks", "torch.int32", self._lists * nb), nb,
+                                    _device(blocks, "blocks", self._int, self._lists * nb), nb,
                                     op)
 
     def select(self, layer: int, q, blocks_out):
@@ -771,4 +778,4 @@ class Rows:
         qp, ldq = self._q(q)
         nb = blocks_out.shape[-1]
         kvr_packed_select(self.h, layer, qp, ldq, nb,
-                          _device(blocks_out, "blocks_out", "torch.int32", self._lists * nb))
+                          _device(blocks_out, "blocks_out", self._int, self._lists * nb))
