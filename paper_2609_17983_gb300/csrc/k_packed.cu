@@ -238,6 +238,9 @@ __device__ __forceinline__ void v_codes_load(const uint8_t *half, int kg, int ch
   }
   transpose_in(h, c);
 }
+__device__ __forceinline__ uint32_t bits(__half2 x) { return *(const uint32_t *)&x; }
+__device__ __forceinline__ __half2 half2_of(uint32_t x) { return *(const __half2 *)&x; }
+
 // Values of eight codes with scale code sc, as halves (exact).
 __device__ __forceinline__ void eight_values(uint32_t c, uint32_t sc, __half2 *v) {
   const uint32_t s2 = sc << 7 | sc << 23;
@@ -285,8 +288,8 @@ __device__ __forceinline__ void block_bounds(float *amax, const uint32_t (*w)[4]
                      s23 = __byte_perm(sc[kt][h], 0, 0x4342) << 7;
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const __half2 two = *(const __half2 *)(b < 2 ? &s01 : &s23),
-                      s2 = b & 1 ? __high2half2(two) : __low2half2(two);
+        const __half2 two = half2_of(b < 2 ? s01 : s23);
+        const __half2 s2 = b & 1 ? __high2half2(two) : __low2half2(two);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const __half2 y = __hmul2(*(const __half2 *)&v[b][2 * h + x], s2);
@@ -298,14 +301,18 @@ __device__ __forceinline__ void block_bounds(float *amax, const uint32_t (*w)[4]
   }
   // lanes apart by 16, 8, 4: each keeps the half of its entries that its bit of lg names
 #pragma unroll
-  for (int n = 4, o = 16; n; n /= 2, o /= 2) {
+  for (int k = 0; k < 3; ++k) {
+    const int n = 4 >> k, o = 16 >> k;
     const bool upper = lane & o;
 #pragma unroll
     for (int i = 0; i < n; ++i) {
-      const __half2 sh = upper ? hi[i] : hi[i + n], sl = upper ? lo[i] : lo[i + n];
-      const __half2 kh = upper ? hi[i + n] : hi[i], kl = upper ? lo[i + n] : lo[i];
-      hi[i] = __hmax2(kh, __shfl_xor_sync(0xFFFFFFFFu, sh, o));
-      lo[i] = __hmin2(kl, __shfl_xor_sync(0xFFFFFFFFu, sl, o));
+      // (of the registers, not of the half2s: choosing between those is choosing between
+      // addresses, and takes the arrays to local memory)
+      const uint32_t h0 = bits(hi[i]), h1 = bits(hi[i + n]), l0 = bits(lo[i]), l1 = bits(lo[i + n]);
+      const uint32_t sh = __shfl_xor_sync(0xFFFFFFFFu, upper ? h0 : h1, o),
+                     sl = __shfl_xor_sync(0xFFFFFFFFu, upper ? l0 : l1, o);
+      hi[i] = __hmax2(half2_of(upper ? h1 : h0), half2_of(sh));
+      lo[i] = __hmin2(half2_of(upper ? l1 : l0), half2_of(sl));
     }
   }
   // lane (lg, lt) holds db 4 d4 + lg / 2, entries 4 lt + 2 (lg & 1) and the next
