@@ -1,5 +1,6 @@
 // k_packed.cu -- the packed cache's rows and blocks: quantising K/V rows as they are
 // written, reading them back, and selecting blocks by their bounds.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include <type_traits>
@@ -721,41 +722,65 @@ __global__ void __launch_bounds__(2 * DH) k_packed_unpack(const UnpackArgs a) {
 
 // ------------------------------------------------------------ block selection
 
-// A CTA per (row, KV head): P_c = sum over the group's heads of max(q, 0), N_c that of
-// min(q, 0) (in head order), both in 8 bits of a common power of two; a block's
-// score is u sum_c (P_c hi_c + N_c lo_c), an upper bound (up to the roundings) of the
-// sum of the heads' largest products with a key of the block.  The sum is of whole
-// numbers below 2^23 and u a power of two, so a score is exact and does not depend on the
-// order of its sum.  The row's own block is always taken; of the earlier ones those with
-// the highest scores, ties to the lowest.
-constexpr int SEL_THREADS = 256;
+// P_c = sum over the group's heads of max(q, 0), N_c that of min(q, 0) (in head order),
+// both in 8 bits of a common power of two; a block's score is u sum_c (P_c hi_c + N_c
+// lo_c), an upper bound (up to the roundings) of the sum of the heads' largest products
+// with a key of the block.  The sum is of whole numbers below 2^23 and u a power of two,
+// so a score is exact and does not depend on the order of its sum.  The row's own
+// block is always taken; of the earlier ones those with the highest scores, ties to the
+// lowest.
+//
+// A cluster of CTAs per (row, KV head), each with a slice of the blocks: eight lanes a
+// block, SEL_AHEAD blocks of a lane in flight from the start (their loads cover those
+// of q).  The scores meet in the first CTA's shared memory, ordered as unsigned
+// numbers; it finds a threshold by bisection (which ends as soon as as many lie above as
+// are wanted) and writes the blocks in order, a warp a stretch of them.
+constexpr int SEL_THREADS = 256, SEL_WARPS = SEL_THREADS / 32, SEL_AHEAD = 4;
 template <int DH, typename T>
 __global__ void __launch_bounds__(SEL_THREADS)
     k_packed_select(const T *q, int ldq, const PackedRow *rows, int layer, int grp, int count,
-                    int32_t *blocks) {
+                    int cl, int32_t *blocks) {
+  constexpr int W = 2 * DH / 8 / 16;  // 16-byte pieces of a block's bounds a lane
   extern __shared__ uint32_t keys[];  // ordered scores of the blocks before the own
   __shared__ __align__(16) int8_t qs[2][DH];
   __shared__ float amax[DH / 32];
-  __shared__ int tot[SEL_THREADS / 32][2];
+  __shared__ uint32_t range[2][SEL_WARPS];
+  __shared__ int tot[2][SEL_WARPS];
+  namespace cg = cooperative_groups;
+  const cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row = blockIdx.x, g = blockIdx.y, G = gridDim.y;
+  const int row = blockIdx.x / cl, rank = blockIdx.x % cl, g = blockIdx.y, G = gridDim.y;
   pdl_trigger();
+  const PackedRow r = rows[row];
   pdl_wait();
-  const int pos = rows[row].pos;
   int32_t *out = blocks + ((size_t)row * G + g) * count;
-  if (pos < 0) {
-    for (int i = tid; i < count; i += SEL_THREADS) out[i] = -1;
+  const int own = r.pos < 0 ? -1 : r.pos / KVR_PAGE;
+  if (own < count) {  // every block that the row sees (the same for all of the cluster)
+    for (int i = tid; i < count && rank == 0; i += SEL_THREADS) out[i] = i <= own ? i : -1;
     return;
   }
-  const PackedView v = rows[row].doc;
-  const int own = pos / KVR_PAGE;
-  if (own + 1 <= count) {  // every block that the row sees
-    for (int i = tid; i < count; i += SEL_THREADS) out[i] = i <= own ? i : -1;
-    return;
-  }
+  const int per = (own + cl - 1) / cl, b0 = rank * per, b1 = min(own, b0 + per);
+  const int sub = lane >> 3, piece = lane & 7;
+  const size_t at = r.doc.index(layer, g, 0);
+  int4 x[SEL_AHEAD][W];
+  float u[SEL_AHEAD];
+  auto fetch = [&](int b) {
+#pragma unroll
+    for (int k = 0; k < SEL_AHEAD; ++k) {
+      const int bk = b + k * 4 * SEL_WARPS;
+      if (bk >= b1) continue;
+      const int4 *p = (const int4 *)(r.doc.bounds + (at + bk) * 2 * DH) + piece * W;
+#pragma unroll
+      for (int i = 0; i < W; ++i) x[k][i] = p[i];
+      u[k] = r.doc.unit[at + bk];
+    }
+  };
+  const int first = b0 + 4 * warp + sub;
+  fetch(first);
   float up = 0.f, down = 0.f;
   if (tid < DH) {
     const T *x = q + (size_t)row * ldq + (size_t)g * grp * DH + tid;
+#pragma unroll 4
     for (int h = 0; h < grp; ++h) {
       const float f = (float)x[h * DH];
       up = __fadd_rn(up, f > 0.f ? f : f != f ? f : 0.f);
@@ -773,66 +798,98 @@ __global__ void __launch_bounds__(SEL_THREADS)
 #pragma unroll
     for (int w = 1; w < DH / 32; ++w) a = fmaxf(a, amax[w]);
     // queries that are not finite score nothing: the lowest blocks are taken
-    const float r = a < INFINITY ? __frcp_rn(unit_of(a)) : 0.f;
-    qs[0][tid] = a < INFINITY ? (int8_t)__float2int_rn(up * r) : 0;
-    qs[1][tid] = a < INFINITY ? (int8_t)__float2int_rn(down * r) : 0;
+    const float f = a < INFINITY ? __frcp_rn(unit_of(a)) : 0.f;
+    qs[0][tid] = a < INFINITY ? (int8_t)__float2int_rn(up * f) : 0;
+    qs[1][tid] = a < INFINITY ? (int8_t)__float2int_rn(down * f) : 0;
   }
   __syncthreads();
-  const size_t at = v.index(layer, g, 0);
-  for (int b = tid; b < own; b += SEL_THREADS) {
-    const int4 *w = (const int4 *)(v.bounds + (at + b) * 2 * DH);
-    const int4 *x = (const int4 *)qs;
-    int s = 0;
+  int4 qv[W];
 #pragma unroll
-    for (int i = 0; i < 2 * DH / 16; ++i) {
-      const int4 a = w[i], c = x[i];
-      s = __dp4a(a.x, c.x, s);
-      s = __dp4a(a.y, c.y, s);
-      s = __dp4a(a.z, c.z, s);
-      s = __dp4a(a.w, c.w, s);
+  for (int i = 0; i < W; ++i) qv[i] = ((const int4 *)qs)[piece * W + i];
+  uint32_t *all = cl > 1 ? cluster.map_shared_rank(keys, 0) : keys;
+  for (int b = first; b - sub - 4 * warp < b1; b += 4 * SEL_WARPS * SEL_AHEAD) {
+    if (b != first) fetch(b);
+#pragma unroll
+    for (int k = 0; k < SEL_AHEAD; ++k) {
+      const int bk = b + k * 4 * SEL_WARPS;
+      int s = 0;
+      if (bk < b1) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          s = __dp4a(x[k][i].x, qv[i].x, s);
+          s = __dp4a(x[k][i].y, qv[i].y, s);
+          s = __dp4a(x[k][i].z, qv[i].z, s);
+          s = __dp4a(x[k][i].w, qv[i].w, s);
+        }
+      }
+#pragma unroll
+      for (int o = 4; o; o /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+      if (bk < b1 && piece == 0) {
+        const float f = (float)s * u[k];
+        const uint32_t v = __float_as_uint(f == 0.f ? 0.f : f);
+        all[bk] = v >> 31 ? ~v : v | 0x80000000u;
+      }
     }
-    const float f = (float)s * v.unit[at + b];
-    const uint32_t u = __float_as_uint(f == 0.f ? 0.f : f);
-    keys[b] = u >> 31 ? ~u : u | 0x80000000u;
   }
-  __syncthreads();
-  // the (count - 1)-th largest key, bit by bit: the largest t with at least that many >= t
+  if (cl > 1) {
+    cluster.sync();
+    if (rank) return;
+  } else {
+    __syncthreads();
+  }
+  // the want-th largest key: the largest t with at least that many >= t
   const int want = count - 1;
-  uint32_t t = 0;
-  for (int bit = 31; bit >= 0 && want > 0; --bit) {
-    const uint32_t c = t | 1u << bit;
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  for (int b = tid; b < own; b += SEL_THREADS) lo = min(lo, keys[b]), hi = max(hi, keys[b]);
+  lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+  hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+  if (lane == 0) range[0][warp] = lo, range[1][warp] = hi;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < SEL_WARPS; ++w) lo = min(lo, range[0][w]), hi = max(hi, range[1][w]);
+  // at least `want` are >= lo, fewer are > hi
+  for (int step = 0; lo < hi && want > 0; step ^= 1) {
+    const uint32_t mid = lo + (hi - lo + 1) / 2;
     int n = 0;
-    for (int b = tid; b < own; b += SEL_THREADS) n += keys[b] >= c;
+    for (int b = tid; b < own; b += SEL_THREADS) n += keys[b] >= mid;
     n = __reduce_add_sync(0xFFFFFFFFu, n);
-    if (lane == 0) tot[warp][bit & 1] = n;
+    if (lane == 0) tot[step][warp] = n;
     __syncthreads();
     n = 0;
 #pragma unroll
-    for (int w = 0; w < SEL_THREADS / 32; ++w) n += tot[w][bit & 1];
-    if (n >= want) t = c;
+    for (int w = 0; w < SEL_WARPS; ++w) n += tot[step][w];
+    if (n >= want) lo = mid;
+    if (n <= want) hi = n == want ? mid : mid - 1;
   }
-  // in order: keys above t, and as many of those equal to it as are wanted
-  if (warp == 0) {
-    int above = 0;
-    for (int b = lane; b < own; b += 32) above += keys[b] > t;
-    above = __reduce_add_sync(0xFFFFFFFFu, above);
-    int ties = want - above, n = 0;
-    for (int b0 = 0; b0 < own && n < want; b0 += 32) {
-      const uint32_t kx = b0 + lane < own ? keys[b0 + lane] : 0;
-      const uint32_t gt = __ballot_sync(0xFFFFFFFFu, b0 + lane < own && kx > t);
-      uint32_t eq = __ballot_sync(0xFFFFFFFFu, b0 + lane < own && kx == t);
-      const uint32_t below = (1u << lane) - 1;
-      const bool take = (gt >> lane & 1) || ((eq >> lane & 1) && __popc(eq & below) < ties);
-      const uint32_t took = __ballot_sync(0xFFFFFFFFu, take);
-      if (take) out[n + __popc(took & below)] = b0 + lane;
-      n += __popc(took);
-      ties -= min(ties, __popc(eq));
-    }
-    if (lane == 0) out[want] = own;
+  const uint32_t t = lo;
+  // keys above t, and as many of those equal to it as are wanted, in order
+  const int span = (own + SEL_WARPS - 1) / SEL_WARPS, w0 = warp * span, w1 = min(own, w0 + span);
+  int gt = 0, eq = 0;
+  for (int b = w0 + lane; b < w1; b += 32) gt += keys[b] > t, eq += keys[b] == t;
+  gt = __reduce_add_sync(0xFFFFFFFFu, gt);
+  eq = __reduce_add_sync(0xFFFFFFFFu, eq);
+  __syncthreads();
+  if (lane == 0) tot[0][warp] = gt, tot[1][warp] = eq;
+  __syncthreads();
+  int above = 0, gts = 0, eqs = 0;  // above t in all, and before this warp's stretch
+#pragma unroll
+  for (int w = 0; w < SEL_WARPS; ++w) {
+    above += tot[0][w];
+    if (w < warp) gts += tot[0][w], eqs += tot[1][w];
   }
+  const int ties = want - above;
+  for (int b = w0; b < w1 && want > 0; b += 32) {
+    const uint32_t kx = b + lane < w1 ? keys[b + lane] : 0, below = (1u << lane) - 1;
+    const uint32_t mg = __ballot_sync(0xFFFFFFFFu, b + lane < w1 && kx > t),
+                   me = __ballot_sync(0xFFFFFFFFu, b + lane < w1 && kx == t);
+    const int e = eqs + __popc(me & below);
+    if ((mg >> lane & 1) || ((me >> lane & 1) && e < ties))
+      out[gts + __popc(mg & below) + min(e, ties)] = b + lane;
+    gts += __popc(mg);
+    eqs += __popc(me);
+  }
+  if (tid == 0) out[want] = own;
 }
-
-PerDevice<size_t> sel_smem[4];
 
 }  // namespace
 
@@ -930,26 +987,45 @@ void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pag
     kernel<<<grid, 2 * v.dh, 0, s>>>(a);
 }
 
+namespace {
+template <int DH, typename T>
+const char *select_blocks(const PackedAttnArgs &a, int max_pages, int32_t *blocks, cudaStream_t s) {
+  static PerDevice<size_t> state;
+  auto *kernel = k_packed_select<DH, T>;
+  const size_t smem = (size_t)max_pages * sizeof(uint32_t);
+  if (smem > 40 * 1024)
+    if (const char *e = smem_opt_in(state, kernel, smem)) return e;
+  // a CTA for every 64 blocks of a row (its warps' loads are in flight at once for 128) as
+  // long as the chip takes them all together
+  int cl = 1;
+  while (cl < 8 && max_pages > 64 * cl && (long long)a.n_rows * a.G * cl * 2 <= 2 * a.num_sms)
+    cl *= 2;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(a.n_rows * cl, a.G);
+  cfg.blockDim = dim3(SEL_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cl;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = g_pdl && a.settled ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, (const T *)a.q, a.ldq, a.rows, a.layer,
+                                           a.grp, a.n_blocks, cl, blocks);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+}  // namespace
+
 const char *launch_packed_select(const PackedAttnArgs &a, int max_pages, int32_t *blocks,
                                  cudaStream_t s) {
-  const size_t smem = (size_t)max_pages * sizeof(uint32_t);
-  const dim3 grid(a.n_rows, a.G);
-  auto run = [&](auto kernel, auto *q, int which) -> const char * {
-    if (smem > 40 * 1024)
-      if (const char *e = smem_opt_in(sel_smem[which], kernel, smem)) return e;
-    const cudaError_t e =
-        launch_pdl(kernel, grid, dim3(SEL_THREADS), smem, s, q, a.ldq, a.rows, a.layer, a.grp,
-                   a.n_blocks, blocks);
-    return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
-  };
-  if (a.dtype == KVR_DTYPE_BF16) {
-    auto *q = (const __nv_bfloat16 *)a.q;
-    return a.dh == 128 ? run(k_packed_select<128, __nv_bfloat16>, q, 0)
-                       : run(k_packed_select<64, __nv_bfloat16>, q, 1);
-  }
-  auto *q = (const float *)a.q;
-  return a.dh == 128 ? run(k_packed_select<128, float>, q, 2)
-                     : run(k_packed_select<64, float>, q, 3);
+  if (a.dtype == KVR_DTYPE_BF16)
+    return a.dh == 128 ? select_blocks<128, __nv_bfloat16>(a, max_pages, blocks, s)
+                       : select_blocks<64, __nv_bfloat16>(a, max_pages, blocks, s);
+  return a.dh == 128 ? select_blocks<128, float>(a, max_pages, blocks, s)
+                     : select_blocks<64, float>(a, max_pages, blocks, s);
 }
 
 }  // namespace kvr

@@ -328,6 +328,7 @@ kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, Pac
   a.settled = r->settled;
   a.n_rows = (int)r->pos.size();
   a.dev_flag = m->dev_flag;
+  a.num_sms = m->num_sms;
   return KVR_OK;
 }
 

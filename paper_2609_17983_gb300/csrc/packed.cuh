@@ -201,6 +201,7 @@ struct PackedAttnArgs {
   float2 *ws_ml;    // [cluster][G][PACK_CLUSTER][PACK_VEC]
   int *counters;    // [tile][G][PACK_CLUSTER], zero between calls
   int *dev_flag;
+  int num_sms;
   bool settled;     // the tables were sent before the kernel that precedes this one
 };
 int packed_attn_ctas_per_sm(int dtype, int warps);  // CTAs of 4, or 12 (fp32: 8), warps
