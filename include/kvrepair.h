@@ -351,6 +351,28 @@ kvr_status kvr_packed_select(kvr_rows *rows, int32_t layer, const void *q, int32
 kvr_status kvr_packed_attention_blocks(kvr_rows *rows, int32_t layer, const void *q, int32_t ldq,
                                        const int32_t *blocks, int32_t n_blocks, void *out);
 
+/* A document's cache in 4 bits: the rows of every position and layer of `cache`
+ * quantised (kvr_packed_write's form), its tokens with them, and room for
+ * a query behind.  The cache itself is not changed and may be freed.  Asynchronous;
+ * allocates.  Errors: KVR_E_INVAL, KVR_E_POISONED, KVR_E_NOMEM, KVR_E_CUDA. */
+kvr_status kvr_pack(const kvr_cache *cache, kvr_packed **out);
+
+/* kvr_repair on a packed document (from kvr_pack): the rows of P are recomputed from the
+ * edited tokens, layer by layer, against the packed entries, and quantised into them
+ * before any of them attends at that layer.  Arguments and errors as
+ * kvr_repair; KVR_E_INVAL for a packed cache without tokens or one that kvr_packed_write
+ * has lengthened. */
+kvr_status kvr_packed_repair(kvr_packed *packed, const int32_t *new_tokens, int32_t edit_start,
+                             int32_t edit_len, const int32_t *positions, int32_t n_positions);
+
+/* kvr_logits on a packed document: the query's m tokens attend, at positions n.., to all
+ * positions (n_blocks == 0) or, in every layer, to the n_blocks blocks that
+ * kvr_packed_select picks for each row.  Their own K/V are quantised behind the document,
+ * whose entries, bounds and length stay as they were.  Synchronous.  Errors as
+ * kvr_logits and kvr_packed_repair; KVR_E_RANGE for n_blocks outside [0, 16384]. */
+kvr_status kvr_packed_logits(kvr_model *model, kvr_packed *packed, const int32_t *query, int32_t m,
+                             int32_t n_blocks, float *logits_out);
+
 /* ---- inspection (tests, benchmarks) ---- */
 
 /* Number of cached positions n. */

@@ -3,6 +3,7 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "packed.cuh"
@@ -335,7 +336,7 @@ __device__ __forceinline__ void block_bounds(float *amax, const uint32_t (*w)[4]
   *(uint16_t *)(bounds + DH + at) = pair(floorf(l.x * r), floorf(l.y * r));
   if (threadIdx.x == 0) *unit = u;
 }
-// The same from a K half in shared memory.
+// The same from a K half in memory.
 template <int DH>
 __device__ __forceinline__ void block_bounds(float *amax, const uint8_t *kb, int present,
                                              int8_t *bounds, float *unit) {
@@ -433,6 +434,17 @@ __global__ void __launch_bounds__(2 * DH, sizeof(T) == 2 ? 512 / DH : 256 / DH)
   if (tid >= DH / 2) return;
   const size_t at = v.index(l0 + l, g, page);
   block_bounds<DH>(amax, kb, present, v.bounds + at * 2 * DH, v.unit + at);
+}
+
+// The bounds of a page alone.  Grid (G, layers), DH / 2 threads.
+template <int DH>
+__global__ void __launch_bounds__(DH / 2) k_packed_bounds(const PackedView v, int page, int present) {
+  __shared__ float amax[2];
+  pdl_trigger();
+  pdl_wait();
+  const size_t at = v.index(blockIdx.y, blockIdx.x, page);
+  block_bounds<DH>(amax, v.block(blockIdx.y, blockIdx.x, page), present, v.bounds + at * 2 * DH,
+                   v.unit + at);
 }
 
 // Pages that a call writes in part: a CTA per (KV head, page, layer).  The new rows are
@@ -971,6 +983,12 @@ void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, 
   by_kind(v.dh, dtype, rows, [&](auto d, auto t, const auto &r) {
     read_rows<decltype(d)::value, decltype(t)>(v, r, l0, nl, k, val, s);
   });
+}
+
+void launch_packed_bounds(const PackedView &v, int page, int len, int nl, cudaStream_t s) {
+  const int present = std::min(KVR_PAGE, len - page * KVR_PAGE);
+  launch_pdl(v.dh == 128 ? k_packed_bounds<128> : k_packed_bounds<64>, dim3(v.G, nl),
+             dim3(v.dh / 2), 0, s, v, page, present);
 }
 
 void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, const void *q,

@@ -287,7 +287,8 @@ struct RopeArgs {
 };
 
 // The row's cache entry (o) and rows_out entry (ro), for a k or v head hh; c
-// null for a query head or a pass that writes no K/V.
+// null for a query head, a pass that writes no K/V, or one whose rows go to rows_out
+// alone.
 template <typename T>
 __device__ __forceinline__ void rope_dst(const RopeArgs &a, int hh, int i, int p, T *&c, size_t &o,
                                          size_t &ro) {
@@ -295,8 +296,8 @@ __device__ __forceinline__ void rope_dst(const RopeArgs &a, int hh, int i, int p
   if (hh >= a.H && a.write_kv) {
     const int kv = hh < a.H + a.G ? 0 : 1, gk = hh - a.H - kv * a.G;
     const KVView v = a.views ? a.views[a.rowdoc[i]] : a.single;
-    c = (T *)v.pages;
-    o = v.offset(a.layer, kv, gk, p);
+    c = (T *)v.pages;  // null: rows_out alone
+    if (c) o = v.offset(a.layer, kv, gk, p);
     // rows_out: K then V, each [M][L][G][dh]
     ro = ((((size_t)kv * a.M + i) * a.L + a.layer) * a.G + gk) * a.dh;
   }
@@ -364,9 +365,11 @@ __global__ void __launch_bounds__(ROPE_HEADS * 64) k_rope_scatter(const RopeArgs
     }
     return;
   }
-  if (!c) return;
-  st(c, o + t, x1);
-  st(c, o + t + half, x2);
+  if (!a.write_kv) return;
+  if (c) {
+    st(c, o + t, x1);
+    st(c, o + t + half, x2);
+  }
   if (a.rows_out) {
     st((T *)a.rows_out, ro + t, x1);
     st((T *)a.rows_out, ro + t + half, x2);
@@ -439,9 +442,11 @@ __global__ void __launch_bounds__(ROPE_THREADS, HPT > 1 ? 4 : 1) k_rope_rows(con
     T *c;
     size_t o = 0, ro = 0;
     rope_dst(a, hh, i, p, c, o, ro);
-    if (!c) continue;
-    st4(c, o + t, y1);
-    st4(c, o + t + half, y2);
+    if (!a.write_kv) continue;
+    if (c) {
+      st4(c, o + t, y1);
+      st4(c, o + t + half, y2);
+    }
     if (a.rows_out) {
       st4((T *)a.rows_out, ro + t, y1);
       st4((T *)a.rows_out, ro + t + half, y2);

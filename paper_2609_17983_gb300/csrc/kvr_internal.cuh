@@ -229,6 +229,7 @@ struct kvr_model {
   std::vector<kvr_cache *> caches;  // live caches, freed with the model
   std::vector<kvr_packed *> packed;  // live packed caches and rows over them, likewise
   std::vector<kvr_rows *> rows;
+  kvr_rows *pass_rows = nullptr;  // the rows of a pass over a packed cache (one of `rows`)
   void *weight_block = nullptr;
   size_t weight_bytes = 0;
   void *embed = nullptr, *lm_head = nullptr;
@@ -521,7 +522,8 @@ void launch_rmsnorm(float *h, const float *g, int row0, int M, int d, double eps
                     int out_dtype, int num_sms, cudaStream_t s, const SplitView *sv = nullptr);
 // q_out: fp32 rotated q; qb_out (optional): bf16 rotated q times qscale;
 // rows_out (optional, with write_kv): the K/V rows as written into the cache,
-// K then V, each [M][L][G][dh] in the cache dtype.
+// K then V, each [M][L][G][dh] in the cache dtype; without pages (single.pages
+// and views null) they go there alone.
 void launch_rope_scatter(const float *qkv, const float2 *rope, const int32_t *pos, int M,
                          const Dims &dm, int layer, const KVView *views, const int32_t *rowdoc,
                          KVView single, float *q_out, void *qb_out, float qscale, bool write_kv,

@@ -296,23 +296,11 @@ kvr_status attn_workspace(kvr_model *m, PackedAttnArgs &a, long long parts, long
   return KVR_OK;
 }
 
-// Checks common to the calls on rows, and what their kernels take.
-kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, PackedAttnArgs &a) {
-  if (!r) return fail(KVR_E_INVAL, "NULL rows");
-  kvr_model *m = r->model;
+// What the kernels of a call on rows take.
+PackedAttnArgs kernel_args(const kvr_rows *r, int layer, const void *q, int ldq) {
+  const kvr_model *m = r->model;
   const Dims &dm = m->dims;
-  if (layer < 0 || layer >= dm.L) return fail(KVR_E_RANGE, "layer %d outside [0, %d)", layer, dm.L);
-  for (const kvr_packed *d : r->docs) {
-    if (!d) return fail(KVR_E_INVAL, "a document of these rows has been freed");
-    if (d->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned");
-  }
-  if (!r->sent) return fail(KVR_E_INVAL, "rows whose last move failed");
-  if (ldq < dm.H * dm.dh || ldq * dm.es() % 16)
-    return fail(KVR_E_INVAL, "row stride %d of q: at least %d, whole 16-byte pieces", ldq,
-                dm.H * dm.dh);
-  KVR_TRY(use_device(m));
-  KVR_TRY(check_device_ptr(m, q, "q"));
-  a = PackedAttnArgs{};
+  PackedAttnArgs a{};
   a.q = q;
   a.ldq = ldq;
   a.dtype = dm.dtype;
@@ -329,10 +317,132 @@ kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, Pac
   a.n_rows = (int)r->pos.size();
   a.dev_flag = m->dev_flag;
   a.num_sms = m->num_sms;
+  return a;
+}
+
+// The same after the checks common to the calls.
+kvr_status rows_args(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, PackedAttnArgs &a) {
+  if (!r) return fail(KVR_E_INVAL, "NULL rows");
+  kvr_model *m = r->model;
+  const Dims &dm = m->dims;
+  if (layer < 0 || layer >= dm.L) return fail(KVR_E_RANGE, "layer %d outside [0, %d)", layer, dm.L);
+  for (const kvr_packed *d : r->docs) {
+    if (!d) return fail(KVR_E_INVAL, "a document of these rows has been freed");
+    if (d->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned");
+  }
+  if (!r->sent) return fail(KVR_E_INVAL, "rows whose last move failed");
+  if (ldq < dm.H * dm.dh || ldq * dm.es() % 16)
+    return fail(KVR_E_INVAL, "row stride %d of q: at least %d, whole 16-byte pieces", ldq,
+                dm.H * dm.dh);
+  KVR_TRY(use_device(m));
+  KVR_TRY(check_device_ptr(m, q, "q"));
+  a = kernel_args(r, layer, q, ldq);
+  return KVR_OK;
+}
+
+// Attention over all positions (a: rows_args').
+kvr_status attend_all(kvr_rows *r, PackedAttnArgs &a, void *out) {
+  kvr_model *m = r->model;
+  const void *q = a.q;
+  const int ldq = a.ldq, layer = a.layer;
+  a.out = out;
+  if (r->n_parts) {
+    KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles));
+    if (const char *e = launch_packed_attention(a, m->stream))
+      return fail(KVR_E_CUDA, "packed attention: %s", e);
+    KVR_TRY(launched(m, 1, "packed attention"));
+    r->settled = true;
+  }
+  const Dims &dm = m->dims;
+  const size_t row_b = (size_t)dm.H * dm.dh * dm.es(), page_b = (size_t)2 * dm.G * KVR_PAGE * dm.dh * 2;
+  for (const kvr_rows::Many &x : r->many) {
+    KVR_TRY(grow_device(m, m->pack_pages, m->pack_pages_bytes, x.plan.pages * page_b,
+                        "unpacked pages"));
+    const size_t q_b = up256(x.plan.rows * row_b);
+    KVR_TRY(grow_device(m, m->pack_q, m->pack_q_bytes, q_b + (size_t)x.plan.rows * dm.H * 4,
+                        "query rows"));
+    float *q_scale = (float *)((char *)m->pack_q + q_b);
+    launch_packed_unpack(r->docs[x.doc]->view(), layer, x.plan.pages, m->pack_pages,
+                         (const char *)q + (size_t)x.row0 * ldq * dm.es(), ldq, dm.H, x.plan.rows,
+                         m->pack_q, q_scale, r->settled, m->stream);
+    KVR_TRY(launched(m, 1, "unpack"));
+    r->settled = true;
+    KVR_TRY(many_attention(m, x.plan, (const int4 *)(r->many_d + x.table), m->pack_q, q_scale,
+                           r->pos_d + x.row0, m->pack_pages, r->identity_d,
+                           (char *)out + x.row0 * row_b));
+  }
+  return KVR_OK;
+}
+
+// The blocks of each row.
+kvr_status select_blocks(kvr_rows *r, PackedAttnArgs &a, int n_blocks, int32_t *blocks_out) {
+  kvr_model *m = r->model;
+  a.n_blocks = n_blocks;
+  if (const char *e = launch_packed_select(a, r->max_pages, blocks_out, m->stream))
+    return fail(KVR_E_CUDA, "block selection: %s", e);
+  KVR_TRY(launched(m, 1, "block selection"));
+  r->settled = true;
+  return KVR_OK;
+}
+
+// Attention over listed blocks.
+kvr_status attend_blocks(kvr_rows *r, PackedAttnArgs &a, const int32_t *blocks, int n_blocks,
+                         void *out) {
+  kvr_model *m = r->model;
+  a.out = out;
+  a.blocks = blocks;
+  a.n_blocks = n_blocks;
+  const long long tiles = (long long)a.n_rows * ((a.grp + PACK_VEC - 1) / PACK_VEC);
+  if (tiles * n_blocks > 0x7FFFFFFF)
+    return fail(KVR_E_UNSUPPORTED, "too many rows (%d) for %d blocks each", a.n_rows, n_blocks);
+  Deal dl = deal(m, {{n_blocks, (int)tiles}}, a.G);
+  dl.per = std::min(dl.per, packed_attn_max_blocks_per_part());
+  a.warps = dl.warps;
+  a.cluster = dl.cluster;
+  a.parts_per_row = dl.parts(n_blocks);
+  KVR_TRY(attn_workspace(m, a, tiles * a.parts_per_row, tiles));
+  if (const char *e = launch_packed_attention(a, m->stream))
+    return fail(KVR_E_CUDA, "block attention: %s", e);
+  KVR_TRY(launched(m, 1, "block attention"));
+  r->settled = true;
   return KVR_OK;
 }
 
 }  // namespace
+
+namespace kvr {
+
+kvr_status packed_rows_of(kvr_model *m, const int32_t *pos, int n, PackedRows &rows) {
+  return rows_of(m, pos, n, rows);
+}
+
+kvr_status packed_pass_rows(kvr_packed *c, const int32_t *pos, int n, kvr_rows **out) {
+  kvr_model *m = c->model;
+  if (!m->pass_rows) {
+    m->pass_rows = new kvr_rows();
+    m->pass_rows->model = m;
+    m->rows.push_back(m->pass_rows);
+  }
+  kvr_rows *r = m->pass_rows;
+  r->docs.assign(1, c);
+  r->doc_rows.assign(1, n);
+  r->pos.assign(pos, pos + n);
+  *out = r;
+  return build_rows(r, r->pos.data());
+}
+
+kvr_status packed_attend(kvr_rows *r, int layer, const void *q, void *out, int n_blocks) {
+  kvr_model *m = r->model;
+  PackedAttnArgs a = kernel_args(r, layer, q, m->dims.H * m->dims.dh);
+  if (!n_blocks) return attend_all(r, a, out);
+  KVR_TRY(grow_device(m, m->sel_scratch, m->sel_scratch_bytes,
+                      (size_t)a.n_rows * a.G * n_blocks * sizeof(int32_t), "selected blocks"));
+  int32_t *blocks = (int32_t *)m->sel_scratch;
+  KVR_TRY(select_blocks(r, a, n_blocks, blocks));
+  return attend_blocks(r, a, blocks, n_blocks, out);
+}
+
+}  // namespace kvr
 
 extern "C" {
 
@@ -375,6 +485,7 @@ void kvr_packed_free(kvr_packed *c) {
   cudaStreamSynchronize(m->stream);
   m->packed.erase(std::remove(m->packed.begin(), m->packed.end(), c), m->packed.end());
   for (kvr_rows *r : m->rows) std::replace(r->docs.begin(), r->docs.end(), c, (kvr_packed *)nullptr);
+  dev_free(c->tokens_d);
   dev_free(c->blocks);
   dev_free(c->bounds);
   dev_free(c->unit);
@@ -499,6 +610,7 @@ void kvr_rows_free(kvr_rows *r) {
   flush_uploads(m);
   cudaStreamSynchronize(m->stream);
   m->rows.erase(std::remove(m->rows.begin(), m->rows.end(), r), m->rows.end());
+  if (m->pass_rows == r) m->pass_rows = nullptr;
   dev_free(r->mem);
   delete r;
 }
@@ -508,33 +620,7 @@ kvr_status kvr_packed_attention(kvr_rows *r, int32_t layer, const void *q, int32
   KVR_TRY(rows_args(r, layer, q, ldq, a));
   kvr_model *m = r->model;
   KVR_TRY(check_device_ptr(m, out, "out"));
-  a.out = out;
-  if (r->n_parts) {
-    KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles));
-    if (const char *e = launch_packed_attention(a, m->stream))
-      return fail(KVR_E_CUDA, "packed attention: %s", e);
-    KVR_TRY(launched(m, 1, "packed attention"));
-    r->settled = true;
-  }
-  const Dims &dm = m->dims;
-  const size_t row_b = (size_t)dm.H * dm.dh * dm.es(), page_b = (size_t)2 * dm.G * KVR_PAGE * dm.dh * 2;
-  for (const kvr_rows::Many &x : r->many) {
-    KVR_TRY(grow_device(m, m->pack_pages, m->pack_pages_bytes, x.plan.pages * page_b,
-                        "unpacked pages"));
-    const size_t q_b = up256(x.plan.rows * row_b);
-    KVR_TRY(grow_device(m, m->pack_q, m->pack_q_bytes, q_b + (size_t)x.plan.rows * dm.H * 4,
-                        "query rows"));
-    float *q_scale = (float *)((char *)m->pack_q + q_b);
-    launch_packed_unpack(r->docs[x.doc]->view(), layer, x.plan.pages, m->pack_pages,
-                         (const char *)q + (size_t)x.row0 * ldq * dm.es(), ldq, dm.H, x.plan.rows,
-                         m->pack_q, q_scale, r->settled, m->stream);
-    KVR_TRY(launched(m, 1, "unpack"));
-    r->settled = true;
-    KVR_TRY(many_attention(m, x.plan, (const int4 *)(r->many_d + x.table), m->pack_q, q_scale,
-                           r->pos_d + x.row0, m->pack_pages, r->identity_d,
-                           (char *)out + x.row0 * row_b));
-  }
-  return KVR_OK;
+  return attend_all(r, a, out);
 }
 
 kvr_status kvr_packed_select(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
@@ -545,12 +631,7 @@ kvr_status kvr_packed_select(kvr_rows *r, int32_t layer, const void *q, int32_t 
     return fail(KVR_E_RANGE, "n_blocks=%d outside [1, %d]", n_blocks, MAX_BLOCKS);
   kvr_model *m = r->model;
   KVR_TRY(check_device_ptr(m, blocks_out, "blocks_out"));
-  a.n_blocks = n_blocks;
-  if (const char *e = launch_packed_select(a, r->max_pages, blocks_out, m->stream))
-    return fail(KVR_E_CUDA, "block selection: %s", e);
-  KVR_TRY(launched(m, 1, "block selection"));
-  r->settled = true;
-  return KVR_OK;
+  return select_blocks(r, a, n_blocks, blocks_out);
 }
 
 kvr_status kvr_packed_attention_blocks(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
@@ -562,23 +643,7 @@ kvr_status kvr_packed_attention_blocks(kvr_rows *r, int32_t layer, const void *q
   kvr_model *m = r->model;
   KVR_TRY(check_device_ptr(m, out, "out"));
   KVR_TRY(check_device_ptr(m, blocks, "blocks"));
-  a.out = out;
-  a.blocks = blocks;
-  a.n_blocks = n_blocks;
-  const long long tiles = (long long)a.n_rows * ((a.grp + PACK_VEC - 1) / PACK_VEC);
-  if (tiles * n_blocks > 0x7FFFFFFF)
-    return fail(KVR_E_UNSUPPORTED, "too many rows (%d) for %d blocks each", a.n_rows, n_blocks);
-  Deal dl = deal(m, {{n_blocks, (int)tiles}}, a.G);
-  dl.per = std::min(dl.per, packed_attn_max_blocks_per_part());
-  a.warps = dl.warps;
-  a.cluster = dl.cluster;
-  a.parts_per_row = dl.parts(n_blocks);
-  KVR_TRY(attn_workspace(m, a, tiles * a.parts_per_row, tiles));
-  if (const char *e = launch_packed_attention(a, m->stream))
-    return fail(KVR_E_CUDA, "block attention: %s", e);
-  KVR_TRY(launched(m, 1, "block attention"));
-  r->settled = true;
-  return KVR_OK;
+  return attend_blocks(r, a, blocks, n_blocks, out);
 }
 
 }  // extern "C"

@@ -241,6 +241,8 @@ void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pag
 struct kvr_packed {
   kvr_model *model = nullptr;
   int n = 0, cap = 0, pages = 0;
+  std::vector<int32_t> tokens_h;  // of a document that was packed (kvr_pack), else empty
+  int32_t *tokens_d = nullptr;    // device [cap]
   uint8_t *blocks = nullptr;
   int8_t *bounds = nullptr;
   float *unit = nullptr;
@@ -271,3 +273,17 @@ struct kvr_rows {
   kvr::PackedRow *rows_d = nullptr;
   int32_t *pos_d = nullptr;
 };
+
+namespace kvr {
+
+// ---- of packed.cu, for the passes of api.cu ----
+kvr_status packed_rows_of(kvr_model *m, const int32_t *pos, int n, PackedRows &rows);
+// The model's own rows over one document, at positions (ascending) that may lie past
+// its length; their tables are queued for upload.
+kvr_status packed_pass_rows(kvr_packed *c, const int32_t *pos, int n, kvr_rows **out);
+// Attention of layer `layer` over all positions, or (n_blocks > 0) the selected blocks.
+kvr_status packed_attend(kvr_rows *r, int layer, const void *q, void *out, int n_blocks);
+// The bounds of one page of layers [0, nl) over its slots below the length len.
+void launch_packed_bounds(const PackedView &v, int page, int len, int nl, cudaStream_t s);
+
+}  // namespace kvr

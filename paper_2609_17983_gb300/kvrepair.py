@@ -106,6 +106,9 @@ _sigs = {
     "kvr_transplant": ([_P, _P, _P, _I32], _I32),
     "kvr_answer_logprob": ([_P, _P, _P, _I32, _P, _I32, _P], _I32),
     "kvr_margin": ([_P, _P, _P, _I32, _P, _I32, _P, _I32, _P], _I32),
+    "kvr_pack": ([_P, ctypes.POINTER(_P)], _I32),
+    "kvr_packed_repair": ([_P, _P, _I32, _I32, _P, _I32], _I32),
+    "kvr_packed_logits": ([_P, _P, _P, _I32, _I32, _P], _I32),
     "kvr_packed_create": ([_P, _I32, ctypes.POINTER(_P)], _I32),
     "kvr_packed_free": ([_P], None),
     "kvr_packed_len": ([_P], _I32),
@@ -300,6 +303,24 @@ def kvr_margin(model, cache, prompt, a_new, a_old) -> float:
 def kvr_packed_create(model, capacity: int) -> ctypes.c_void_p:
     out = ctypes.c_void_p()
     _check(_lib.kvr_packed_create(model, capacity, ctypes.byref(out)))
+    return out
+
+
+def kvr_pack(cache) -> ctypes.c_void_p:
+    out = ctypes.c_void_p()
+    _check(_lib.kvr_pack(cache, ctypes.byref(out)))
+    return out
+
+
+def kvr_packed_repair(packed, new_tokens, edit_start: int, positions):
+    nt, ps = _i32(new_tokens), _i32(positions)
+    _check(_lib.kvr_packed_repair(packed, _ptr(nt), edit_start, nt.size, _ptr(ps), ps.size))
+
+
+def kvr_packed_logits(model, packed, query, vocab: int, n_blocks: int = 0) -> np.ndarray:
+    q = _i32(query)
+    out = np.zeros(vocab, np.float32)
+    _check(_lib.kvr_packed_logits(model, packed, _ptr(q), q.size, n_blocks, out.ctypes.data))
     return out
 
 
@@ -559,6 +580,14 @@ class Model:
         """An empty packed cache (4 bits an entry) for up to `capacity` positions."""
         return Packed(self, kvr_packed_create(self.h, capacity))
 
+    def pack(self, cache: "Cache") -> "Packed":
+        """The document's cache in 4 bits (kvr_pack); the cache may be closed then."""
+        return Packed(self, kvr_pack(cache.h))
+
+    def packed_logits(self, packed: "Packed", query, n_blocks: int = 0) -> np.ndarray:
+        """logits over a packed document; n_blocks > 0: each row attends to that many blocks."""
+        return kvr_packed_logits(self.h, packed.h, query, self.cfg["vocab"], n_blocks)
+
     def rows(self, docs) -> "Rows":
         """Query rows over packed documents; docs: list of (Packed, positions)."""
         return Rows(self, docs)
@@ -706,6 +735,10 @@ class Packed:
     def read(self, positions, k_out, v_out, layer_begin: int = 0, layer_end: int | None = None):
         """The stored rows into k_out and v_out (kvr_packed_read)."""
         kvr_packed_read(self.h, *self._rows(positions, layer_begin, layer_end, k_out, v_out))
+
+    def repair(self, new_tokens, edit_start: int, positions):
+        """Repair the packed document in place (kvr_packed_repair)."""
+        kvr_packed_repair(self.h, new_tokens, edit_start, positions)
 
     def bounds(self, layer: int = 0):
         """hi, lo [n_kv_heads][blocks][head_dim] (int8) and unit [n_kv_heads][blocks]."""
