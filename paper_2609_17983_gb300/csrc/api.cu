@@ -989,7 +989,8 @@ bool many_plan(const kvr_model *m, const int32_t *pos, int rows, std::vector<int
 }
 
 kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, const void *q,
-                          const float *q_scale, const int32_t *pos, void *pages, const int32_t *identity, void *out) {
+                          int ldq, const int32_t *pos, void *pages, const int32_t *identity,
+                          void *out) {
   Dims dm = m->dims;
   dm.L = 1;  // the pages hold one layer
   CUtensorMap tm;
@@ -999,10 +1000,10 @@ kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, c
   const char *e =
       p.n_pairs ? launch_attention_pair(q, pos, tables, p.n_blocks, tables + p.n_blocks, p.n_pairs,
                                         p.splits, dm, 0, identity, tm, m->attn_ws_o, m->attn_ws_ml,
-                                        out, m->dev_flag, m->stream, nullptr, nullptr, q_scale)
+                                        out, m->dev_flag, m->stream, nullptr, nullptr, ldq)
                 : launch_attention_tc5(q, pos, tables, p.n_blocks, p.splits, dm, 0, pages, identity,
                                        tm, m->attn_ws_o, m->attn_ws_ml, out, m->dev_flag, m->stream,
-                                       nullptr, nullptr, NO_TAIL, 0, q_scale);
+                                       nullptr, nullptr, NO_TAIL, 0, ldq);
   if (!e)
     e = launch_attention_combine(tables, p.n_blocks, p.block_rows, p.splits, dm, m->attn_ws_o,
                                  m->attn_ws_ml, out, m->stream);
@@ -1056,7 +1057,6 @@ void kvr_model_free(kvr_model *m) {
   dev_free(m->pack_ws);
   dev_free(m->pack_count);
   dev_free(m->pack_pages);
-  dev_free(m->pack_q);
   dev_free(m->tcw.counters);
   dev_free(m->blocks_d);
   dev_free(m->attn_ws_o);

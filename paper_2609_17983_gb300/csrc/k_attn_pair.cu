@@ -54,9 +54,9 @@ constexpr uint32_t TMEM_COLS = 512;  // S0, S1 (128 columns each; P over the fir
 constexpr float RESCALE_LOG2 = 8.f;  // headroom of the reference maximum (P <= 2^8)
 
 struct PairParams {
-  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE (HALF: halves)
+  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE (HALF: rows ldq apart)
+  int ldq;
   float qk_scale;          // log2(e) / sqrt(dh): scores into the log2 domain
-  const float *q_scale;    // HALF: [M][H], what q was divided by
   const int32_t *pos;      // [M] ascending per document
   const int4 *blocks;      // tiles: (row0, nrows, kmax, doc)
   const int4 *pairs;       // (first tile, tiles: 1 or 2, kmax of the pair, doc)
@@ -346,12 +346,24 @@ __global__ void __launch_bounds__(NT, 1)
       return r != 0;
     };
     pdl_wait();
+    float qk_scale = p.qk_scale;
     {  // half a row of Q into the swizzled tile: 128-byte rows, 16-byte pieces XORed by row
       constexpr int QP = DH / 8 / KP;  // 16-byte pieces of this thread
-      const uint4 *src = (const uint4 *)(p.q + ((size_t)row * p.H + hh) * DH) + part * QP;
+      const size_t at = HALF ? (size_t)row * p.ldq + hh * DH : ((size_t)row * p.H + hh) * DH;
+      const uint4 *src = (const uint4 *)(p.q + at) + part * QP;
       uint4 x[QP];
 #pragma unroll
       for (int k = 0; k < QP; ++k) x[k] = real ? src[k] : make_uint4(0u, 0u, 0u, 0u);
+      if (HALF) {
+        float m = 0.f;
+#pragma unroll
+        for (int k = 0; k < QP; ++k) m = fmaxf(m, bf16_magnitude(x[k]));
+        m = hand_over(m, [](float a, float b) { return fmaxf(a, b); });
+        const int e = half_exponent(m);
+#pragma unroll
+        for (int k = 0; k < QP; ++k) x[k] = halves_of(x[k], exp2_of(-e));
+        qk_scale *= exp2_of(e);
+      }
       const uint32_t q0 = sQ + t * QBYTES + v * 128;
 #pragma unroll
       for (int k = 0; k < QP; ++k) {
@@ -362,8 +374,6 @@ __global__ void __launch_bounds__(NT, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_full);
     }
-    float qk_scale = p.qk_scale;
-    if (HALF && real) qk_scale *= p.q_scale[(size_t)row * p.H + hh];
     float m = -INFINITY, l = 0.f;  // reference maximum, this half's sum of exponentials
     bool dead = false;             // warp-uniform: a wait ran out
     for (int i = 0; i < n; ++i) {
@@ -541,12 +551,12 @@ const char *launch_attention_pair(const void *q, const int32_t *pos, const int4 
                                   const Dims &dm, int layer, const int32_t *table,
                                   const CUtensorMap &tm_kv, float *ws_o, float2 *ws_ml, void *out,
                                   int *dev_flag, cudaStream_t s, const KVView *views,
-                                  const CUtensorMap *tmaps, const float *q_scale) {
+                                  const CUtensorMap *tmaps, int half_ldq) {
   if (n_pairs <= 0) return nullptr;
   if ((views == nullptr) != (tmaps == nullptr)) return "document views without tensor maps";
   PairParams p{};
   p.q = (const __nv_bfloat16 *)q;
-  p.q_scale = q_scale;
+  p.ldq = half_ldq;
   p.qk_scale = (float)(1.4426950408889634 / std::sqrt((double)dm.dh));
   p.pos = pos;
   p.blocks = blocks;
@@ -566,9 +576,9 @@ const char *launch_attention_pair(const void *q, const int32_t *pos, const int4 
   p.out = (__nv_bfloat16 *)out;
   p.dev_flag = dev_flag;
   if (dm.dh == 128)
-    return q_scale ? run<128, true>(tm_kv, p, n_pairs, s) : run<128, false>(tm_kv, p, n_pairs, s);
+    return half_ldq ? run<128, true>(tm_kv, p, n_pairs, s) : run<128, false>(tm_kv, p, n_pairs, s);
   if (dm.dh == 64)
-    return q_scale ? run<64, true>(tm_kv, p, n_pairs, s) : run<64, false>(tm_kv, p, n_pairs, s);
+    return half_ldq ? run<64, true>(tm_kv, p, n_pairs, s) : run<64, false>(tm_kv, p, n_pairs, s);
   return "head_dim not supported";
 }
 

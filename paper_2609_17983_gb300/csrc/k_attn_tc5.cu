@@ -69,9 +69,9 @@ constexpr float RESCALE_LOG2 = 8.f;  // headroom of the reference maximum (P <= 
 constexpr int KV_STAGES = 4;
 
 struct Attn5Params {
-  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE (HALF: halves)
+  const __nv_bfloat16 *q;  // [M][H * dh] post-RoPE (HALF: rows ldq apart)
+  int ldq;
   float qk_scale;          // log2(e) / sqrt(dh): scores into the log2 domain
-  const float *q_scale;    // HALF: [M][H], what q was divided by
   const int32_t *pos;      // [M] ascending (one document)
   const int4 *blocks;      // (row0, nrows, kmax, doc)
   const __nv_bfloat16 *pages;  // the cache's page pool (one document)
@@ -340,22 +340,36 @@ __global__ void __launch_bounds__(NT5, 1)
       asm volatile("bar.sync %0, %1;" ::"r"(bar_id), "n"(32 * SMW) : "memory");
     };
     pdl_wait();
+    float qk_scale = p.qk_scale;
     // this thread's part of the Q row (DH / SMW elements, zero past the
     // block's query vectors) into the TMEM lane of query vector v
     {
       constexpr int QW = DH / (2 * SMW);  // 32-bit words (columns) of this part
       const bool real = v < mq;
-      const uint4 *src = (const uint4 *)(p.q + ((size_t)(row0 + (real ? v / p.grp : 0)) * p.H +
-                                                g * p.grp + v % p.grp) * DH) +
-                         part * (QW / 4);
+      const int row = row0 + (real ? v / p.grp : 0), head = g * p.grp + v % p.grp;
+      const size_t at = HALF ? (size_t)row * p.ldq + head * DH : ((size_t)row * p.H + head) * DH;
+      const uint4 *src = (const uint4 *)(p.q + at) + part * (QW / 4);
       uint32_t w[QW];
+      float mq_part = 0.f;
 #pragma unroll
       for (int k = 0; k < QW / 4; ++k) {
         const uint4 x = real ? src[k] : make_uint4(0u, 0u, 0u, 0u);
+        if (HALF) mq_part = fmaxf(mq_part, bf16_magnitude(x));
         w[4 * k] = x.x;
         w[4 * k + 1] = x.y;
         w[4 * k + 2] = x.z;
         w[4 * k + 3] = x.w;
+      }
+      if (HALF) {  // the parts' largest magnitudes make the row's
+        sx[0][part][v] = mq_part;
+        quad_bar();
+#pragma unroll
+        for (int o = 0; o < SMW; ++o) mq_part = fmaxf(mq_part, sx[0][o][v]);
+        quad_bar();
+        const int e = half_exponent(mq_part);
+#pragma unroll
+        for (int k = 0; k < QW; ++k) w[k] = halves_of(w[k], exp2_of(-e));
+        qk_scale *= exp2_of(e);
       }
 #pragma unroll
       for (int k = 0; k < QW / 8; ++k) tmem_st8_nowait(tl + T_Q + part * QW + k * 8, w + 8 * k);
@@ -367,9 +381,6 @@ __global__ void __launch_bounds__(NT5, 1)
     constexpr int HK = CH / SMW;  // keys of this thread per chunk
     constexpr int OC = DH / SMW;  // O columns of this thread
     const int pv = spos[v];
-    float qk_scale = p.qk_scale;
-    if (HALF && v < mq)
-      qk_scale *= p.q_scale[(size_t)(row0 + v / p.grp) * p.H + g * p.grp + v % p.grp];
     float m = -INFINITY, l = 0.f;  // reference maximum, this part's sum of exponentials
     bool dead = false;             // warp-uniform: a wait ran out
     for (int i = 0; i < nch; ++i) {
@@ -581,7 +592,7 @@ const char *launch_attention_tc5(const void *q, const int32_t *pos, const int4 *
                                  float *ws_o, float2 *ws_ml, void *out, int *dev_flag,
                                  cudaStream_t s, const KVView *views,
                                  const CUtensorMap *tmaps, int tail_page, int tail_docs,
-                                 const float *q_scale) {
+                                 int half_ldq) {
   if (n_blocks <= 0) return nullptr;
   if ((views == nullptr) != (tmaps == nullptr)) return "document views without tensor maps";
   if (!views && tail_page != NO_TAIL) return "a tail without document views";
@@ -591,7 +602,7 @@ const char *launch_attention_tc5(const void *q, const int32_t *pos, const int4 *
   p.tail_page = tail_page;
   p.tail_docs = tail_docs;
   p.q = (const __nv_bfloat16 *)q;
-  p.q_scale = q_scale;
+  p.ldq = half_ldq;
   p.qk_scale = (float)(1.4426950408889634 / std::sqrt((double)dm.dh));
   p.pos = pos;
   p.blocks = blocks;
@@ -608,8 +619,8 @@ const char *launch_attention_tc5(const void *q, const int32_t *pos, const int4 *
   p.ws_ml = ws_ml;
   p.out = (__nv_bfloat16 *)out;
   p.dev_flag = dev_flag;
-  if (dm.dh == 128) return q_scale ? run<128, true>(tm_kv, p, s) : run<128, false>(tm_kv, p, s);
-  if (dm.dh == 64) return q_scale ? run<64, true>(tm_kv, p, s) : run<64, false>(tm_kv, p, s);
+  if (dm.dh == 128) return half_ldq ? run<128, true>(tm_kv, p, s) : run<128, false>(tm_kv, p, s);
+  if (dm.dh == 64) return half_ldq ? run<64, true>(tm_kv, p, s) : run<64, false>(tm_kv, p, s);
   return "head_dim not supported";
 }
 

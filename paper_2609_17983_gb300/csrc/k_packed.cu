@@ -654,56 +654,17 @@ __global__ void __launch_bounds__(2 * DH)
   }
 }
 
-// What the attention of many rows reads, in halves (both exact).  Grid (G, pages + q's
-// CTAs): a CTA per (KV head, page) widens the block into pages [page][K, V][G][KVR_PAGE][DH];
-// the others take UNPACK_Q vectors (row, head) of q a warp, each divided by a power of two
-// that brings its largest magnitude into [2^8, 2^9).
-constexpr int UNPACK_Q = 4;
-struct UnpackArgs {
-  PackedView v;
-  int layer, n_pages;
-  __half *pages;
-  const __nv_bfloat16 *q;
-  int ldq, H, n_vec;
-  __half *q_out;
-  float *q_scale;
-};
+// A CTA per (KV head, page): the block widened (exactly) into pages of halves [page][K, V]
+// [G][KVR_PAGE][DH].
 template <int DH>
-__global__ void __launch_bounds__(2 * DH) k_packed_unpack(const UnpackArgs a) {
-  constexpr int NT = 2 * DH, CH = DH / 8, HB = pack_half_bytes(DH), PER = DH / 32;
+__global__ void __launch_bounds__(2 * DH)
+    k_packed_unpack(const PackedView v, int layer, __half *pages) {
+  constexpr int NT = 2 * DH, CH = DH / 8, HB = pack_half_bytes(DH);
   __shared__ __align__(16) uint8_t blk[2 * HB];
   const int tid = threadIdx.x, g = blockIdx.x, page = blockIdx.y, G = gridDim.x;
   pdl_trigger();
   pdl_wait();
-  if (page >= a.n_pages) {
-    const int lane = tid & 31;
-    const long long v0 = ((long long)((page - a.n_pages) * G + g) * (NT / 32) + (tid >> 5)) * UNPACK_Q;
-    float x[UNPACK_Q][PER];
-#pragma unroll
-    for (int i = 0; i < UNPACK_Q; ++i) {
-      const long long vec = min(v0 + i, (long long)a.n_vec - 1), row = vec / a.H;
-      const __nv_bfloat16 *src = a.q + row * a.ldq + (vec - row * a.H) * DH + PER * lane;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) x[i][j] = __bfloat162float(src[j]);
-    }
-#pragma unroll
-    for (int i = 0; i < UNPACK_Q; ++i) {
-      float m = 0.f;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) m = fmaxf(m, fabsf(x[i][j]));
-#pragma unroll
-      for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-      const int e = pack_q_exponent(m);
-      const float down = pack_exp2(-e);
-      if (v0 + i >= a.n_vec) break;
-      __half *dst = a.q_out + (v0 + i) * DH + PER * lane;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) dst[j] = __float2half_rn(x[i][j] * down);
-      if (lane == 0) a.q_scale[v0 + i] = pack_exp2(e);
-    }
-    return;
-  }
-  const uint8_t *src = a.v.block(a.layer, g, page);
+  const uint8_t *src = v.block(layer, g, page);
   for (int i = tid; i < 2 * HB / 16; i += NT) ((uint4 *)blk)[i] = ((const uint4 *)src)[i];
   __syncthreads();
   const int kg = tid / CH, ch = tid % CH;
@@ -726,7 +687,7 @@ __global__ void __launch_bounds__(2 * DH) k_packed_unpack(const UnpackArgs a) {
                         : pack_k_scale(DH, 4 * kg + j, ch >> 1);
       __align__(16) __half2 y[4];
       eight_values(c[j], bad[j] ? (kv ? 0 : PACK_NAN) : half[at], y);
-      *(uint4 *)(a.pages + ((((size_t)page * 2 + kv) * G + g) * KVR_PAGE + 4 * kg + j) * DH +
+      *(uint4 *)(pages + ((((size_t)page * 2 + kv) * G + g) * KVR_PAGE + 4 * kg + j) * DH +
                  8 * ch) = *(const uint4 *)y;
     }
   }
@@ -991,18 +952,14 @@ void launch_packed_bounds(const PackedView &v, int page, int len, int nl, cudaSt
              dim3(v.dh / 2), 0, s, v, page, present);
 }
 
-void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, const void *q,
-                          int ldq, int H, int rows, void *q_out, float *q_scale, bool settled,
+void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, bool settled,
                           cudaStream_t s) {
   auto *kernel = v.dh == 128 ? k_packed_unpack<128> : k_packed_unpack<64>;
-  const int per = v.G * (2 * v.dh / 32) * UNPACK_Q;  // vectors of a line of CTAs
-  const dim3 grid(v.G, n_pages + (rows * H + per - 1) / per);
-  const UnpackArgs a{v, layer, n_pages, (__half *)pages, (const __nv_bfloat16 *)q, ldq, H, rows * H,
-                     (__half *)q_out, q_scale};
+  const dim3 grid(v.G, n_pages);
   if (settled)
-    launch_pdl(kernel, grid, dim3(2 * v.dh), 0, s, a);
+    launch_pdl(kernel, grid, dim3(2 * v.dh), 0, s, v, layer, (__half *)pages);
   else
-    kernel<<<grid, 2 * v.dh, 0, s>>>(a);
+    kernel<<<grid, 2 * v.dh, 0, s>>>(v, layer, (__half *)pages);
 }
 
 namespace {

@@ -282,8 +282,6 @@ struct kvr_model {
   size_t pack_count_bytes = 0;
   void *pack_pages = nullptr;  // a layer's pages of a document, unpacked for many rows
   size_t pack_pages_bytes = 0;
-  void *pack_q = nullptr;      // and its queries, in halves
-  size_t pack_q_bytes = 0;
   int *dev_flag = nullptr;     // device error flag (bounded waits)
   kvr::TraceBuf trace{};       // attached device timeline buffer, if any
   kvr::SplitView pending{};    // split tiles of h not yet added (next RMSNorm adds them)
@@ -659,8 +657,8 @@ const char *launch_attention_combine(const int4 *blocks, int n_blocks, int max_r
 // and tm_kv (its TMA view).  Several: views and tmaps, device arrays indexed
 // by a block's document (blocks[].w), tmaps 64-byte aligned.  tail_page: logical pages
 // from it on lie in another pool, with view and TMA view tail_docs entries further.
-// q_scale (both kernels): q and the pages are halves, row r's head h divided by
-// q_scale[r][h]; P is rounded to a half then.
+// half_ldq > 0 (both kernels): the pages are halves, q's rows (bf16) half_ldq entries
+// apart; q goes as halves scaled by a power of two, and P is rounded to a half.
 int attn_tc5_rows_per_block(int grp);
 int attn_tc5_ctas_per_sm(int dh);
 constexpr int NO_TAIL = 0x7fffffff;
@@ -670,7 +668,7 @@ const char *launch_attention_tc5(const void *q, const int32_t *pos, const int4 *
                                  float *ws_o, float2 *ws_ml, void *out, int *dev_flag,
                                  cudaStream_t s, const KVView *views = nullptr,
                                  const CUtensorMap *tmaps = nullptr, int tail_page = NO_TAIL,
-                                 int tail_docs = 0, const float *q_scale = nullptr);
+                                 int tail_docs = 0, int half_ldq = 0);
 
 // The same over many rows: the blocks are tiles of at most
 // attn_tc5_rows_per_block(grp) rows, and each CTA takes a pair (device int4:
@@ -681,8 +679,7 @@ const char *launch_attention_pair(const void *q, const int32_t *pos, const int4 
                                   const Dims &dm, int layer, const int32_t *table,
                                   const CUtensorMap &tm_kv, float *ws_o, float2 *ws_ml, void *out,
                                   int *dev_flag, cudaStream_t s, const KVView *views = nullptr,
-                                  const CUtensorMap *tmaps = nullptr,
-                                  const float *q_scale = nullptr);
+                                  const CUtensorMap *tmaps = nullptr, int half_ldq = 0);
 
 // ---- kernels: selectors ----
 // The keys of a simple policy (EditLocal, Structural, Random,

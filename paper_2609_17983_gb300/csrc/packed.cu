@@ -358,16 +358,12 @@ kvr_status attend_all(kvr_rows *r, PackedAttnArgs &a, void *out) {
   for (const kvr_rows::Many &x : r->many) {
     KVR_TRY(grow_device(m, m->pack_pages, m->pack_pages_bytes, x.plan.pages * page_b,
                         "unpacked pages"));
-    const size_t q_b = up256(x.plan.rows * row_b);
-    KVR_TRY(grow_device(m, m->pack_q, m->pack_q_bytes, q_b + (size_t)x.plan.rows * dm.H * 4,
-                        "query rows"));
-    float *q_scale = (float *)((char *)m->pack_q + q_b);
-    launch_packed_unpack(r->docs[x.doc]->view(), layer, x.plan.pages, m->pack_pages,
-                         (const char *)q + (size_t)x.row0 * ldq * dm.es(), ldq, dm.H, x.plan.rows,
-                         m->pack_q, q_scale, r->settled, m->stream);
+    launch_packed_unpack(r->docs[x.doc]->view(), layer, x.plan.pages, m->pack_pages, r->settled,
+                         m->stream);
     KVR_TRY(launched(m, 1, "unpack"));
     r->settled = true;
-    KVR_TRY(many_attention(m, x.plan, (const int4 *)(r->many_d + x.table), m->pack_q, q_scale,
+    KVR_TRY(many_attention(m, x.plan, (const int4 *)(r->many_d + x.table),
+                           (const char *)q + (size_t)x.row0 * ldq * dm.es(), ldq,
                            r->pos_d + x.row0, m->pack_pages, r->identity_d,
                            (char *)out + x.row0 * row_b));
   }

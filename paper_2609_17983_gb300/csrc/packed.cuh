@@ -130,15 +130,6 @@ __device__ __forceinline__ float pack_scale(uint32_t code) {
   return __half2float(__ushort_as_half((unsigned short)(code << 7)));
 }
 
-// 2^e for e in [-126, 127], and the power of two that brings magnitudes up to a (finite)
-// into [2^8, 2^9): what it then leaves below a half's range is below 2^-32 of a.
-__device__ __forceinline__ float pack_exp2(int e) {
-  return __uint_as_float((uint32_t)(127 + e) << 23);
-}
-__device__ __forceinline__ int pack_q_exponent(float a) {
-  return min(max((int)(__float_as_uint(a) >> 23) - 127, -100), 126) - 8;
-}
-
 // ---- kernels (k_packed.cu, k_packed_attn.cu) ----
 
 // Positions of a call in segments of one page each: a run of consecutive positions, or
@@ -227,12 +218,10 @@ struct ManyPlan {
 bool many_plan(const kvr_model *m, const int32_t *pos, int rows, std::vector<int32_t> &tables,
                ManyPlan &p);
 kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, const void *q,
-                          const float *q_scale, const int32_t *pos, void *pages, const int32_t *identity, void *out);
-// The first n_pages blocks of a layer as such pages, in halves, and q [rows][H][dh] as
-// halves, each head of a row divided by its q_scale [rows][H].  A key row stored as NaN,
+                          int ldq, const int32_t *pos, void *pages, const int32_t *identity, void *out);
+// The first n_pages blocks of a layer as such pages, in halves.  A key row stored as NaN,
 // or whose value row is, becomes NaN; NaN value rows become zero.
-void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, const void *q,
-                          int ldq, int H, int rows, void *q_out, float *q_scale, bool settled,
+void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, bool settled,
                           cudaStream_t s);
 
 }  // namespace kvr

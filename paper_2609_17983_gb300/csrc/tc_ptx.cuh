@@ -5,9 +5,38 @@
 
 #include <cstdint>
 #include <cuda.h>
+#include <cuda_fp16.h>
 
 namespace kvr {
 namespace ptx {
+
+// 2^e for e in [-126, 127], and the exponent e whose 2^-e brings magnitudes up to a (finite)
+// into [2^8, 2^9): bf16 entries are halves then as exactly as they were bf16, but for
+// those below 2^-32 of a.
+__device__ __forceinline__ float exp2_of(int e) {
+  return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+__device__ __forceinline__ int half_exponent(float a) {
+  return min(max((int)(__float_as_uint(a) >> 23) - 127, -100), 126) - 8;
+}
+// The largest magnitude of eight bf16 (a NaN is passed over), and two as halves times f.
+__device__ __forceinline__ float bf16_magnitude(uint4 x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = fmaxf(m, fmaxf(fabsf(__uint_as_float(w[i] << 16)),
+                       fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+  return m;
+}
+__device__ __forceinline__ uint32_t halves_of(uint32_t w, float f) {
+  const __half2 r = __floats2half2_rn(__uint_as_float(w << 16) * f,
+                                      __uint_as_float(w & 0xFFFF0000u) * f);
+  return *(const uint32_t *)&r;
+}
+__device__ __forceinline__ uint4 halves_of(uint4 x, float f) {
+  return make_uint4(halves_of(x.x, f), halves_of(x.y, f), halves_of(x.z, f), halves_of(x.w, f));
+}
 
 constexpr uint64_t WAIT_NS = 2000000000ull;  // a wait longer than 2 s is a fault
 
