@@ -243,8 +243,8 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
     x.slot = (int)parts.size();
     x.n_parts = dl.parts(t.page1);
     for (x.part = 0; x.part < x.n_parts; ++x.part) {
-      x.page0 = std::min(t.page1, x.part * dl.per);
-      x.page1 = std::min(t.page1, x.page0 + dl.per);
+      x.page0 = (int)((long long)t.page1 * x.part / x.n_parts);
+      x.page1 = (int)((long long)t.page1 * (x.part + 1) / x.n_parts);
       parts.push_back(x);
     }
   }
