@@ -133,14 +133,14 @@ struct Deal {
 };
 
 // The deal whose launch is modelled to end first, in units of 10 ns.  A wave of CTAs costs
-// 5.2 us beside its rounds (a page for each of a CTA's warps), a round 1.35 and 0.1 per
-// warp that shares the SM; a cluster's sums 0.9, a merge through memory 3.1 and 0.04 per
-// cluster; clusters of 4 and 8 leave 1/20 and 1/4 of the SMs without a place.  Fitted to
-// 6900 launches of 1 to 64 rows over 64 to 131072 positions: the deal taken is 1.4% slower
+// 4.9 us beside its rounds (a page for each of a CTA's warps), a round 1.6 and 0.08 per
+// busy warp of the SM; a cluster's sums 1.3, a merge through memory 3.4 and 0.07 per
+// cluster; clusters of 4 and 8 leave 1/20 and 3/8 of the SMs without a place.  Fitted to
+// 6900 launches of 1 to 64 rows over 64 to 131072 positions: the deal taken is 0.9% slower
 // than the fastest on average, 15% at most.  One token over 5000 positions, 4 KV heads: 8
-// CTAs of 12 warps as a cluster 7.4 us (merged through memory 9.2, with 4 warps 8.6); over
-// 131072, 8 KV heads: 19 CTAs of 12 warps a head 32.3 (clusters of 4 34.2); 16 documents
-// of 8191: a CTA a document and head 32.6 (split in two 43.6).
+// CTAs of 12 warps as a cluster 7.0 us (merged through memory 9.2, with 4 warps 8.6); over
+// 131072, 8 KV heads: 19 CTAs of 12 warps a head 32.4 (clusters of 4 34.2); 16 documents
+// of 8191: a CTA a document and head 32.4 (split in two 43.6).
 Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int G) {
   const int many = m->dims.dtype == KVR_DTYPE_BF16 ? 12 : 8;
   int most = 1;
@@ -156,12 +156,13 @@ Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int
         long long ctas = 0;
         for (const auto &x : pages) ctas += (long long)d.parts(x.first) * x.second * G;
         const long long slots = std::max<long long>(
-            cl, (long long)m->num_sms * per_sm * (cl == 8 ? 15 : cl == 4 ? 19 : 20) / 20);
+            cl, (long long)m->num_sms * per_sm * (cl == 8 ? 25 : cl == 4 ? 38 : 40) / 40);
         const long long waves = (ctas + slots - 1) / slots;
         const long long here = std::min<long long>(per_sm, (ctas + m->num_sms - 1) / m->num_sms);
-        const int deep = (std::min(d.per, most) + W - 1) / W, nc = d.parts(most) / cl;
-        const long long t = waves * (520 + deep * (135 + 10 * W * here)) + (cl > 1 ? 90 : 0) +
-                            (nc > 1 ? 310 + 4 * nc : 0);
+        const int parts = d.parts(most), nc = parts / cl, each = (most + parts - 1) / parts;
+        const int deep = std::max(1, (each + W - 1) / W), busy = std::min(W, each);
+        const long long t = waves * (490 + deep * (160 + 8 * busy * here)) + (cl > 1 ? 130 : 0) +
+                            (nc > 1 ? 340 + 7 * nc : 0);
         if (least < 0 || t < least) least = t, best = d;
       }
       if (W * rounds >= most) break;
