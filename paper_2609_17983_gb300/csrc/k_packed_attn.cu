@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
   int done = 0;
   for (; done < n_my; ++done) {
     const int st = done % STAGES;
-    const uint8_t *kb = ring + st * 2 * HB, *vb = kb + HB;
+    uint8_t *kb = ring + st * 2 * HB, *vb = kb + HB;
     bool ok = mbar_wait(&full[warp][st][0], done / STAGES & 1, abort_v, p.dev_flag, 1 << 12);
     if (!__all_sync(0xFFFFFFFFu, ok)) break;
     float s[4][4];
@@ -322,8 +322,6 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
       }
     }
     const int first = page(done) * KVR_PAGE;
-    __syncwarp();
-    if (lane == 0 && done + STAGES < n_my) fetch(done + STAGES, 0);
     ok = mbar_wait(&full[warp][st][1], done / STAGES & 1, abort_v, p.dev_flag, 1 << 13);
     if (!__all_sync(0xFFFFFFFFu, ok)) break;
     // scores; masked keys get none
@@ -351,9 +349,19 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
         uint32_t *x = (uint32_t *)(vb + CB) + i;
         *x &= ~__vcmpeq4(*x, 0xFFFFFFFFu);
       }
-      // before the copy that follows into this memory
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
+    }
+    __syncwarp();
+    // V's scales as halves, once for the eight lanes that take each, where K was
+    uint4 *vs16 = (uint4 *)kb;  // [pairs of tiles 0 1, 2 3][db][t]
+    if (lane < 4 * DB) {
+      const uint4 c4 = *(const uint4 *)(vb + CB + lane * 16);
+      uint4 x, y;
+      scales(c4.x, x.x, x.y);
+      scales(c4.y, x.z, x.w);
+      scales(c4.z, y.x, y.y);
+      scales(c4.w, y.z, y.w);
+      vs16[lane] = x;
+      vs16[4 * DB + lane] = y;
     }
     if (first + KVR_PAGE - 1 > least) {
 #pragma unroll
@@ -416,18 +424,19 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
         l[1] = t[1];
       }
     }
+    __syncwarp();
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
       const uint4 w4 = *(const uint4 *)(vb + (b * 32 + (lane ^ b)) * 16);
-      const uint4 c4 = *(const uint4 *)(vb + CB + (b * 4 + lt) * 16);
-      const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w}, vs[4] = {c4.x, c4.y, c4.z, c4.w};
+      const uint4 x4 = vs16[b * 4 + lt], y4 = vs16[4 * DB + b * 4 + lt];
+      const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+      const uint32_t vs[8] = {x4.x, x4.y, x4.z, x4.w, y4.x, y4.y, y4.z, y4.w};
       float acc[4] = {0.f, 0.f, 0.f, 0.f};
       float *d = SPLIT ? acc : o[b];
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
-        uint32_t a[4], s0, s1;
-        scales(vs[kt], s0, s1);
-        v_fragment(w[kt], s0, s1, a);
+        uint32_t a[4];
+        v_fragment(w[kt], vs[2 * kt], vs[2 * kt + 1], a);
         mma16816(d, a, ph[kt][0], ph[kt][1]);
         if (SPLIT) mma16816(d, a, pl[kt][0], pl[kt][1]);
       }
@@ -436,8 +445,13 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
         for (int i = 0; i < 4; ++i) o[b][i] += acc[i];
       }
     }
+    // what was written here comes before the copies into the same memory
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
-    if (lane == 0 && done + STAGES < n_my) fetch(done + STAGES, 1);
+    if (lane == 0 && done + STAGES < n_my) {
+      fetch(done + STAGES, 0);
+      fetch(done + STAGES, 1);
+    }
   }
   // after a wait that ran out: the copies in flight end before the memory is reused
   if (done < n_my)
