@@ -451,11 +451,12 @@ __global__ void __launch_bounds__(DH / 2) k_packed_bounds(const PackedView v, in
 // quantised, K and V side by side in a warp, into shared memory, while the block's K
 // codes are on their way to registers and so are the V codes of the first groups of four
 // keys that change; words with a new key are patched and stored, and the bounds taken
-// over all rows present.  NT: DH / 2 threads for a few rows (the bounds' warps alone,
-// whose registers then hold all they need; 40 rows of 40 pages, 112 CTAs each: 28.6 us
-// by 2 DH threads), 2 DH for many.  which: the segments of a run that are not whole
-// pages (a list's are blockIdx.y).
-constexpr int PATCH_FEW = 4;
+// over all rows present.  NT: DH / 2 threads for up to PATCH_FEW rows a page (the bounds'
+// warps alone, whose registers then hold all they need), 2 DH for more.  28 layers, 4 KV
+// heads: 40 rows of 40 pages 11.9 us (by 2 DH threads 25), 320 of 40 pages 16.5 (31), 480 of
+// 15 pages 21.3 (22.6), of 10 pages 26.9 (22.1).  which: the segments of a run that are not
+// whole pages (a list's are blockIdx.y).
+constexpr int PATCH_FEW = 32;
 template <int DH, typename T, class Rows, int NT>
 __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
     k_packed_patch(const PackedView v, const __grid_constant__ Rows rows, int2 which, int len,
