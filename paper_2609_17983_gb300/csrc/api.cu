@@ -1804,48 +1804,52 @@ kvr_status kvr_logits(kvr_model *m, const kvr_cache *c, const int32_t *query, in
 }
 
 kvr_status kvr_pack(const kvr_cache *c, kvr_packed **out) {
-  if (!c || !out) return fail(KVR_E_INVAL, "NULL argument");
-  *out = nullptr;
-  if (c->poisoned) return fail(KVR_E_POISONED, "cache poisoned");
-  kvr_model *m = c->model;
-  const Dims &dm = m->dims;
   kvr_packed *p = nullptr;
-  KVR_TRY(kvr_packed_create(m, c->n + KVR_QUERY_RESERVE, &p));
-  const StageScope scope{m};
-  p->tokens_h.assign(c->tokens_h.begin(), c->tokens_h.begin() + c->n);
-  p->tokens_d = (int32_t *)dev_alloc((size_t)p->cap * 4);
-  // layers in groups of about 64 MB of K, gathered into the readback scratch
-  const size_t layer_b = (size_t)c->n * dm.G * dm.dh * dm.es();
-  const int per = (int)std::max<size_t>(1, std::min<size_t>(dm.L, ((size_t)64 << 20) / layer_b));
-  auto al = [](size_t x) { return (x + 255) / 256 * 256; };
-  const size_t pos_b = al((size_t)c->n * 4), row_b = al(per * layer_b);
-  kvr_status st = p->tokens_d ? KVR_OK : fail(KVR_E_NOMEM, "tokens of %d positions", c->n);
-  if (!st)
-    st = grow_scratch(m, m->read_scratch, m->read_scratch_bytes, pos_b + 2 * row_b, "pack scratch");
-  if (!st) st = upload_words(m, p->tokens_d, p->tokens_h.data(), c->n);
-  std::vector<int32_t> pos(c->n);
-  for (int i = 0; i < c->n; ++i) pos[i] = i;
-  char *base = (char *)m->read_scratch;
-  if (!st) st = upload_words(m, base, pos.data(), c->n);
-  PackedRows rows;
-  if (!st) st = packed_rows_of(m, pos.data(), c->n, rows);  // a run: no table
-  void *k = base + pos_b, *v = base + pos_b + row_b;
-  for (int l = 0; l < dm.L && !st; l += per) {
-    const int l1 = std::min(dm.L, l + per);
-    launch_cache_gather_raw(c->view(), dm.dtype, nullptr, (const int32_t *)base, c->n, l, l1, dm.G,
-                            dm.dh, k, v, m->stream);
-    st = launch_check(m, 1);
-    if (st) break;
-    const int n = launch_packed_write(p->view(), dm.dtype, rows, c->n, l, l1 - l, k, v, m->stream);
-    st = launch_check(m, n);
-  }
-  if (st) {
-    kvr_packed_free(p);
-    return st;
-  }
-  p->n = c->n;
-  *out = p;
-  return KVR_OK;
+  return guarded([&]() -> kvr_status {
+    if (!c || !out) return fail(KVR_E_INVAL, "NULL argument");
+    *out = nullptr;
+    if (c->poisoned) return fail(KVR_E_POISONED, "cache poisoned");
+    kvr_model *m = c->model;
+    const Dims &dm = m->dims;
+    KVR_TRY(kvr_packed_create(m, c->n + KVR_QUERY_RESERVE, &p));
+    const StageScope scope{m};
+    p->tokens_h.assign(c->tokens_h.begin(), c->tokens_h.begin() + c->n);
+    p->tokens_d = (int32_t *)dev_alloc((size_t)p->cap * 4);
+    // layers in groups of about 64 MB of K, gathered into the readback scratch
+    const size_t layer_b = (size_t)c->n * dm.G * dm.dh * dm.es();
+    const int per = (int)std::max<size_t>(1, std::min<size_t>(dm.L, ((size_t)64 << 20) / layer_b));
+    auto al = [](size_t x) { return (x + 255) / 256 * 256; };
+    const size_t pos_b = al((size_t)c->n * 4), row_b = al(per * layer_b);
+    kvr_status st = p->tokens_d ? KVR_OK : fail(KVR_E_NOMEM, "tokens of %d positions", c->n);
+    if (!st)
+      st = grow_scratch(m, m->read_scratch, m->read_scratch_bytes, pos_b + 2 * row_b,
+                        "pack scratch");
+    if (!st) st = upload_words(m, p->tokens_d, p->tokens_h.data(), c->n);
+    std::vector<int32_t> pos(c->n);
+    for (int i = 0; i < c->n; ++i) pos[i] = i;
+    char *base = (char *)m->read_scratch;
+    if (!st) st = upload_words(m, base, pos.data(), c->n);
+    PackedRows rows;
+    if (!st) st = packed_rows_of(m, pos.data(), c->n, rows);  // a run: no table
+    void *k = base + pos_b, *v = base + pos_b + row_b;
+    for (int l = 0; l < dm.L && !st; l += per) {
+      const int l1 = std::min(dm.L, l + per);
+      launch_cache_gather_raw(c->view(), dm.dtype, nullptr, (const int32_t *)base, c->n, l, l1,
+                              dm.G, dm.dh, k, v, m->stream);
+      st = launch_check(m, 1);
+      if (st) break;
+      const int n =
+          launch_packed_write(p->view(), dm.dtype, rows, c->n, l, l1 - l, k, v, m->stream);
+      st = launch_check(m, n);
+    }
+    if (st) {
+      kvr_packed_free(p);
+      return st;
+    }
+    p->n = c->n;
+    *out = p;
+    return KVR_OK;
+  }, [&] { kvr_packed_free(p); });
 }
 
 // The pass of rows at P over packed document c, whose tokens there are staged.  len: the
@@ -1877,87 +1881,92 @@ static kvr_status check_packed_document(const kvr_packed *c) {
   if (c->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned by an earlier CUDA error");
   if (!c->tokens_d) return fail(KVR_E_INVAL, "a packed cache without tokens (not from kvr_pack)");
   if (c->n != (int)c->tokens_h.size())
-    return fail(KVR_E_INVAL, "rows were written past the document's %zu tokens", c->tokens_h.size());
+    return fail(KVR_E_INVAL, "rows were written past the document's %zu tokens",
+                c->tokens_h.size());
   return KVR_OK;
 }
 
 kvr_status kvr_packed_repair(kvr_packed *c, const int32_t *new_tokens, int32_t edit_start,
                              int32_t edit_len, const int32_t *positions, int32_t n_positions) {
-  KVR_TRY(check_packed_document(c));
-  kvr_model *m = c->model;
-  const Dims &dm = m->dims;
-  if (edit_len < 0 || n_positions < 0) return fail(KVR_E_RANGE, "negative length");
-  if ((edit_len > 0 && !new_tokens) || (n_positions > 0 && !positions))
-    return fail(KVR_E_INVAL, "NULL argument");
-  if (edit_start < 0 || edit_start > c->n || edit_len > c->n - edit_start)
-    return fail(KVR_E_RANGE, "edit of %d at %d outside [0, %d)", edit_len, edit_start, c->n);
-  const int s_end = edit_start + edit_len;
-  for (int i = 0; i < edit_len; ++i)
-    if (new_tokens[i] < 0 || new_tokens[i] >= dm.V)
-      return fail(KVR_E_RANGE, "new token %d outside [0, %d)", new_tokens[i], dm.V);
-  for (int i = 0; i < n_positions; ++i)
-    if (positions[i] < s_end || positions[i] >= c->n || (i && positions[i] <= positions[i - 1]))
-      return fail(KVR_E_RANGE, "position %d: strictly increasing in [%d, %d) wanted", positions[i],
-                  s_end, c->n);
-  if ((long long)edit_len + n_positions > dm.max_rows)
-    return fail(KVR_E_UNSUPPORTED, "|P|=%d above max_rows", edit_len + n_positions);
-  KVR_TRY(use_device(m));
-  std::vector<int32_t> P(edit_len);
-  for (int i = 0; i < edit_len; ++i) P[i] = edit_start + i;
-  P.insert(P.end(), positions, positions + n_positions);
-  if (P.empty()) return KVR_OK;
-  const StageScope scope{m};
-  bool launched = false;
-  kvr_status st = stage_add(m, c->tokens_d + edit_start, new_tokens, edit_len);
-  if (!st) st = packed_pass(c, P, c->n, 0, true, launched);
-  if (!st)
-    std::copy(new_tokens, new_tokens + edit_len, c->tokens_h.begin() + edit_start);
-  else if (launched || st == KVR_E_CUDA ||
-           (edit_len &&
-            stage_h2d(m, c->tokens_d + edit_start, c->tokens_h.data() + edit_start, edit_len)))
-    c->poisoned = true;
-  return st;
+  return guarded([&]() -> kvr_status {
+    KVR_TRY(check_packed_document(c));
+    kvr_model *m = c->model;
+    const Dims &dm = m->dims;
+    if (edit_len < 0 || n_positions < 0) return fail(KVR_E_RANGE, "negative length");
+    if ((edit_len > 0 && !new_tokens) || (n_positions > 0 && !positions))
+      return fail(KVR_E_INVAL, "NULL argument");
+    if (edit_start < 0 || edit_start > c->n || edit_len > c->n - edit_start)
+      return fail(KVR_E_RANGE, "edit of %d at %d outside [0, %d)", edit_len, edit_start, c->n);
+    const int s_end = edit_start + edit_len;
+    for (int i = 0; i < edit_len; ++i)
+      if (new_tokens[i] < 0 || new_tokens[i] >= dm.V)
+        return fail(KVR_E_RANGE, "new token %d outside [0, %d)", new_tokens[i], dm.V);
+    for (int i = 0; i < n_positions; ++i)
+      if (positions[i] < s_end || positions[i] >= c->n || (i && positions[i] <= positions[i - 1]))
+        return fail(KVR_E_RANGE, "position %d: strictly increasing in [%d, %d) wanted",
+                    positions[i], s_end, c->n);
+    if ((long long)edit_len + n_positions > dm.max_rows)
+      return fail(KVR_E_UNSUPPORTED, "|P|=%d above max_rows", edit_len + n_positions);
+    KVR_TRY(use_device(m));
+    std::vector<int32_t> P(edit_len);
+    for (int i = 0; i < edit_len; ++i) P[i] = edit_start + i;
+    P.insert(P.end(), positions, positions + n_positions);
+    if (P.empty()) return KVR_OK;
+    const StageScope scope{m};
+    bool launched = false;
+    kvr_status st = stage_add(m, c->tokens_d + edit_start, new_tokens, edit_len);
+    if (!st) st = packed_pass(c, P, c->n, 0, true, launched);
+    if (!st)
+      std::copy(new_tokens, new_tokens + edit_len, c->tokens_h.begin() + edit_start);
+    else if (launched || st == KVR_E_CUDA ||
+             (edit_len &&
+              stage_h2d(m, c->tokens_d + edit_start, c->tokens_h.data() + edit_start, edit_len)))
+      c->poisoned = true;
+    return st;
+  }, [&] { if (c) c->poisoned = true; });
 }
 
 kvr_status kvr_packed_logits(kvr_model *m, kvr_packed *c, const int32_t *query, int32_t qm,
                              int32_t n_blocks, float *logits_out) {
-  if (!m || !query || !logits_out) return fail(KVR_E_INVAL, "NULL argument");
-  KVR_TRY(check_packed_document(c));
-  if (c->model != m) return fail(KVR_E_INVAL, "packed cache of another model");
-  const Dims &dm = m->dims;
-  if (qm < 1 || qm > KVR_QUERY_RESERVE || c->n + qm > c->cap)
-    return fail(KVR_E_RANGE, "query length %d outside [1, %d]", qm, KVR_QUERY_RESERVE);
-  if (n_blocks < 0 || n_blocks > 16384)
-    return fail(KVR_E_RANGE, "n_blocks=%d outside [0, 16384]", n_blocks);
-  for (int i = 0; i < qm; ++i)
-    if (query[i] < 0 || query[i] >= dm.V) return fail(KVR_E_RANGE, "query token out of range");
-  KVR_TRY(use_device(m));
-  std::vector<int32_t> P(qm);
-  for (int i = 0; i < qm; ++i) P[i] = c->n + i;
-  const StageScope scope{m};
-  bool launched = false;
-  kvr_status st = stage_add(m, c->tokens_d + c->n, query, qm);
-  if (!st) st = packed_pass(c, P, c->n + qm, n_blocks, false, launched);
-  // the bounds of the document's last block were taken with the query's rows
-  if (launched && c->n % KVR_PAGE) {
-    launch_packed_bounds(c->view(), c->n / KVR_PAGE, c->n, dm.L, m->stream);
-    const kvr_status s2 = launch_check(m, 1);
-    if (!st) st = s2;
-  }
-  if (st && launched) c->poisoned = true;
-  KVR_TRY(st);
-  {
-    Prof pr(m, P_NORM, (int64_t)dm.d * 4);
-    launch_rmsnorm(m->h, m->final_norm, qm - 1, 1, dm.d, dm.eps, m->a, dm.dtype, m->num_sms,
-                   m->stream, &m->pending);
-    m->pending = SplitView{};
-    KVR_TRY(launch_check(m, 1));
-  }
-  KVR_TRY(gemm(m, P_LMHEAD, m->a, m->lm_head, m->tc_lm ? &m->tm_lm : nullptr, nullptr, m->logits,
-               1, dm.V, dm.d, GEMM_EPI_STORE));
-  CUDA_TRY(cudaMemcpyAsync(logits_out, m->logits, (size_t)dm.V * 4, cudaMemcpyDeviceToHost,
-                           m->stream));
-  return sync_model(m);
+  return guarded([&]() -> kvr_status {
+    if (!m || !query || !logits_out) return fail(KVR_E_INVAL, "NULL argument");
+    KVR_TRY(check_packed_document(c));
+    if (c->model != m) return fail(KVR_E_INVAL, "packed cache of another model");
+    const Dims &dm = m->dims;
+    if (qm < 1 || qm > KVR_QUERY_RESERVE || c->n + qm > c->cap)
+      return fail(KVR_E_RANGE, "query length %d outside [1, %d]", qm, KVR_QUERY_RESERVE);
+    if (n_blocks < 0 || n_blocks > 16384)
+      return fail(KVR_E_RANGE, "n_blocks=%d outside [0, 16384]", n_blocks);
+    for (int i = 0; i < qm; ++i)
+      if (query[i] < 0 || query[i] >= dm.V) return fail(KVR_E_RANGE, "query token out of range");
+    KVR_TRY(use_device(m));
+    std::vector<int32_t> P(qm);
+    for (int i = 0; i < qm; ++i) P[i] = c->n + i;
+    const StageScope scope{m};
+    bool launched = false;
+    kvr_status st = stage_add(m, c->tokens_d + c->n, query, qm);
+    if (!st) st = packed_pass(c, P, c->n + qm, n_blocks, false, launched);
+    // the bounds of the document's last block were taken with the query's rows
+    if (launched && c->n % KVR_PAGE) {
+      launch_packed_bounds(c->view(), c->n / KVR_PAGE, c->n, dm.L, m->stream);
+      const kvr_status s2 = launch_check(m, 1);
+      if (!st) st = s2;
+    }
+    if (st && launched) c->poisoned = true;
+    KVR_TRY(st);
+    {
+      Prof pr(m, P_NORM, (int64_t)dm.d * 4);
+      launch_rmsnorm(m->h, m->final_norm, qm - 1, 1, dm.d, dm.eps, m->a, dm.dtype, m->num_sms,
+                     m->stream, &m->pending);
+      m->pending = SplitView{};
+      KVR_TRY(launch_check(m, 1));
+    }
+    KVR_TRY(gemm(m, P_LMHEAD, m->a, m->lm_head, m->tc_lm ? &m->tm_lm : nullptr, nullptr, m->logits,
+                 1, dm.V, dm.d, GEMM_EPI_STORE));
+    CUDA_TRY(cudaMemcpyAsync(logits_out, m->logits, (size_t)dm.V * 4, cudaMemcpyDeviceToHost,
+                             m->stream));
+    return sync_model(m);
+  }, [&] { if (c) c->poisoned = true; });
 }
 
 kvr_status kvr_select(kvr_model *m, const kvr_cache *c, kvr_policy policy, int32_t K,

@@ -10,6 +10,7 @@
 //                  the order of the products' A fragments: a 16-byte load is four
 //                  fragments, each four conversions of two codes and four products with
 //                  the scales, which are exact in half;
+//                  (V's scales are widened once a page, into the memory that K has left);
 //   softmax        over the lane's own keys: the reference of a vector is raised only
 //                  when a score exceeds it by 8 in the log2 domain, so a page costs a
 //                  vote instead of a reduction; the sums stay apart until the end;
@@ -20,6 +21,16 @@
 // The warps' (max, sum, O) meet in shared memory, those of a cluster's CTAs in one
 // another's shared memory, each adding a slice; of several clusters the last to arrive
 // adds them all, in order.
+//
+// The floor is the cache's bytes: one token over 131072 positions of 8 KV heads reads 151 MB,
+// 22.3 us at the copy rate, and takes 31.5; sixteen documents of 8191 positions the same
+// in 31.1.  Of that about 5 us are the launch, the first copy's way and the sums; between
+// them an SM's 12 warps take 12 pages in 2.5 us, 6.7 TB/s over the chip, while its
+// schedulers issue half the time (1000 instructions a page and warp, 450 of them
+// conversions and byte permutations in the ALU's half-rate pipe).  mma.sync serves because
+// eight columns are all there is: with 128 rows of a tcgen05 tile a token's heads
+// would leave 120 empty, and the widened keys would have to pass through shared memory.
+// Many rows go that way (many_attention).
 //
 // A key whose row held a NaN or an infinity has NaN scales: its score is NaN for the
 // vectors that see it, and its V scales are cleared before the products, so
@@ -43,9 +54,8 @@ constexpr int SPARSE_MAX = 128;     // listed blocks of a part
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes,
                                           uint64_t *bar) {
   asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-          su32(dst)),
-      "l"(src), "r"(bytes), "r"(su32(bar))
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+      ::"r"(su32(dst)), "l"(src), "r"(bytes), "r"(su32(bar))
       : "memory");
 }
 

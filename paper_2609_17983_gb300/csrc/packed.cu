@@ -12,6 +12,7 @@ using namespace kvr;
 
 namespace {
 
+static_assert(KVR_BLOCK == KVR_PAGE, "a block is a page");
 constexpr int MAX_CAPACITY = 1 << 20;  // positions of a packed cache
 constexpr int MAX_ROWS = 1 << 20, MAX_DOCS = 4096, MAX_BLOCKS = MAX_CAPACITY / KVR_PAGE;
 
@@ -186,7 +187,8 @@ bool many_rows(const kvr_model *m, const int32_t *pos, int rows, size_t docs) {
   for (int v = 0; v < rows * grp; v += PACK_VEC)
     units += pos[std::min(rows * grp - 1, v + PACK_VEC - 1) / grp] / KVR_PAGE + 1;
   const long long n = pos[rows - 1] + 1;
-  return units * dm.G > (docs > 1 ? 5000 : 0) + (dm.dh == 128 ? 5600 + n * 16 / 25 : 6500 + n * 9 / 10);
+  const long long least = dm.dh == 128 ? 5600 + n * 16 / 25 : 6500 + n * 9 / 10;
+  return units * dm.G > least + (docs > 1 ? 5000 : 0);
 }
 
 // The tables of rows at `pos`, built and sent.
@@ -239,10 +241,12 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   }
   const Deal dl = deal(m, count, dm.G);
   std::vector<PackedPart> parts;
+  bool merged = false;
   for (const PackedPart &t : tiles) {
     PackedPart x = t;
     x.slot = (int)parts.size();
     x.n_parts = dl.parts(t.page1);
+    merged = merged || x.n_parts > dl.cluster;
     for (x.part = 0; x.part < x.n_parts; ++x.part) {
       x.page0 = (int)((long long)t.page1 * x.part / x.n_parts);
       x.page1 = (int)((long long)t.page1 * (x.part + 1) / x.n_parts);
@@ -271,6 +275,7 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   r->n_parts = (int)parts.size();
   r->n_tiles = (int)tiles.size();
   r->max_pages = most;
+  r->merged = merged;
   r->warps = dl.warps;
   r->cluster = dl.cluster;
   std::copy(pos, pos + M, r->pos.begin());
@@ -278,8 +283,11 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   return KVR_OK;
 }
 
-// Room for the partial sums and arrival counts of a launch.
-kvr_status attn_workspace(kvr_model *m, PackedAttnArgs &a, long long parts, long long tiles) {
+// Room for the partial sums and arrival counts of a launch, where a tile has more than one
+// cluster's to add.
+kvr_status attn_workspace(kvr_model *m, PackedAttnArgs &a, long long parts, long long tiles,
+                          bool merged) {
+  if (!merged) return KVR_OK;
   const size_t sums = (size_t)(parts / a.cluster) * a.G,
                o = up256(sums * PACK_VEC * a.dh * sizeof(float)),
                ml = sums * PACK_CLUSTER * PACK_VEC * sizeof(float2),
@@ -348,14 +356,15 @@ kvr_status attend_all(kvr_rows *r, PackedAttnArgs &a, void *out) {
   const int ldq = a.ldq, layer = a.layer;
   a.out = out;
   if (r->n_parts) {
-    KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles));
+    KVR_TRY(attn_workspace(m, a, r->n_parts, r->n_tiles, r->merged));
     if (const char *e = launch_packed_attention(a, m->stream))
       return fail(KVR_E_CUDA, "packed attention: %s", e);
     KVR_TRY(launched(m, 1, "packed attention"));
     r->settled = true;
   }
   const Dims &dm = m->dims;
-  const size_t row_b = (size_t)dm.H * dm.dh * dm.es(), page_b = (size_t)2 * dm.G * KVR_PAGE * dm.dh * 2;
+  const size_t row_b = (size_t)dm.H * dm.dh * dm.es(),
+               page_b = (size_t)2 * dm.G * KVR_PAGE * dm.dh * 2;
   for (const kvr_rows::Many &x : r->many) {
     KVR_TRY(grow_device(m, m->pack_pages, m->pack_pages_bytes, x.plan.pages * page_b,
                         "unpacked pages"));
@@ -397,7 +406,7 @@ kvr_status attend_blocks(kvr_rows *r, PackedAttnArgs &a, const int32_t *blocks, 
   a.warps = dl.warps;
   a.cluster = dl.cluster;
   a.parts_per_row = dl.parts(n_blocks);
-  KVR_TRY(attn_workspace(m, a, tiles * a.parts_per_row, tiles));
+  KVR_TRY(attn_workspace(m, a, tiles * a.parts_per_row, tiles, a.parts_per_row > a.cluster));
   if (const char *e = launch_packed_attention(a, m->stream))
     return fail(KVR_E_CUDA, "block attention: %s", e);
   KVR_TRY(launched(m, 1, "block attention"));
@@ -444,34 +453,37 @@ kvr_status packed_attend(kvr_rows *r, int layer, const void *q, void *out, int n
 extern "C" {
 
 kvr_status kvr_packed_create(kvr_model *m, int32_t capacity, kvr_packed **out) {
-  if (!m || !out) return fail(KVR_E_INVAL, "NULL argument");
-  *out = nullptr;
-  if (capacity < 1 || capacity > MAX_CAPACITY)
-    return fail(KVR_E_RANGE, "capacity %d outside [1, %d]", capacity, MAX_CAPACITY);
-  KVR_TRY(use_device(m));
-  const Dims &dm = m->dims;
-  kvr_packed *c = new kvr_packed();
-  c->model = m;
-  c->cap = capacity;
-  c->pages = (capacity + KVR_PAGE - 1) / KVR_PAGE;
-  const size_t n = (size_t)dm.L * dm.G * c->pages, block_b = n * pack_block_bytes(dm.dh),
-               bound_b = n * 2 * dm.dh;
-  c->blocks = (uint8_t *)dev_alloc(block_b);
-  c->bounds = (int8_t *)dev_alloc(bound_b);
-  c->unit = (float *)dev_alloc(n * sizeof(float));
-  m->packed.push_back(c);
-  if (!c->blocks || !c->bounds || !c->unit) {
-    kvr_packed_free(c);
-    return fail(KVR_E_NOMEM, "packed cache of %d positions", capacity);
-  }
-  if (cudaMemsetAsync(c->blocks, 0, block_b, m->stream) != cudaSuccess ||
-      cudaMemsetAsync(c->bounds, 0, bound_b, m->stream) != cudaSuccess ||
-      cudaMemsetAsync(c->unit, 0, n * sizeof(float), m->stream) != cudaSuccess) {
-    kvr_packed_free(c);
-    return fail(KVR_E_CUDA, "packed cache clear");
-  }
-  *out = c;
-  return KVR_OK;
+  kvr_packed *c = nullptr;
+  return guarded([&]() -> kvr_status {
+    if (!m || !out) return fail(KVR_E_INVAL, "NULL argument");
+    *out = nullptr;
+    if (capacity < 1 || capacity > MAX_CAPACITY)
+      return fail(KVR_E_RANGE, "capacity %d outside [1, %d]", capacity, MAX_CAPACITY);
+    KVR_TRY(use_device(m));
+    const Dims &dm = m->dims;
+    c = new kvr_packed();
+    c->model = m;
+    m->packed.push_back(c);
+    c->cap = capacity;
+    c->pages = (capacity + KVR_PAGE - 1) / KVR_PAGE;
+    const size_t n = (size_t)dm.L * dm.G * c->pages, block_b = n * pack_block_bytes(dm.dh),
+                 bound_b = n * 2 * dm.dh;
+    c->blocks = (uint8_t *)dev_alloc(block_b);
+    c->bounds = (int8_t *)dev_alloc(bound_b);
+    c->unit = (float *)dev_alloc(n * sizeof(float));
+    if (!c->blocks || !c->bounds || !c->unit) {
+      kvr_packed_free(c);
+      return fail(KVR_E_NOMEM, "packed cache of %d positions", capacity);
+    }
+    if (cudaMemsetAsync(c->blocks, 0, block_b, m->stream) != cudaSuccess ||
+        cudaMemsetAsync(c->bounds, 0, bound_b, m->stream) != cudaSuccess ||
+        cudaMemsetAsync(c->unit, 0, n * sizeof(float), m->stream) != cudaSuccess) {
+      kvr_packed_free(c);
+      return fail(KVR_E_CUDA, "packed cache clear");
+    }
+    *out = c;
+    return KVR_OK;
+  }, [&] { kvr_packed_free(c); });
 }
 
 void kvr_packed_free(kvr_packed *c) {
@@ -481,7 +493,8 @@ void kvr_packed_free(kvr_packed *c) {
   flush_uploads(m);
   cudaStreamSynchronize(m->stream);
   m->packed.erase(std::remove(m->packed.begin(), m->packed.end(), c), m->packed.end());
-  for (kvr_rows *r : m->rows) std::replace(r->docs.begin(), r->docs.end(), c, (kvr_packed *)nullptr);
+  for (kvr_rows *r : m->rows)
+    std::replace(r->docs.begin(), r->docs.end(), c, (kvr_packed *)nullptr);
   dev_free(c->tokens_d);
   dev_free(c->blocks);
   dev_free(c->bounds);
@@ -493,111 +506,125 @@ int32_t kvr_packed_len(const kvr_packed *c) { return c ? c->n : -1; }
 
 kvr_status kvr_packed_write(kvr_packed *c, const int32_t *positions, int32_t n_pos, int32_t l0,
                             int32_t l1, const void *k, const void *v) {
-  if (!c) return fail(KVR_E_INVAL, "NULL packed cache");
-  if (c->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned by an earlier CUDA error");
-  kvr_model *m = c->model;
-  KVR_TRY(check_range(m, positions, n_pos, l0, l1, c->cap));
-  for (int i = 0, end = c->n; i < n_pos; ++i) {
-    if (positions[i] > end)
-      return fail(KVR_E_RANGE, "position %d leaves a gap after %d", positions[i], end);
-    end = std::max(end, positions[i] + 1);
-  }
-  if (n_pos == 0 || l0 == l1) return KVR_OK;
-  KVR_TRY(use_device(m));
-  KVR_TRY(check_device_ptr(m, k, "k"));
-  KVR_TRY(check_device_ptr(m, v, "v"));
-  PackedRows rows;
-  KVR_TRY(rows_of(m, positions, n_pos, rows));
-  const int len = std::max(c->n, positions[n_pos - 1] + 1);
-  const int n = launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->stream);
-  const kvr_status st = launched(m, n, "packed write");
-  if (st)
-    c->poisoned = true;
-  else
-    c->n = len;
-  return st;
+  return guarded([&]() -> kvr_status {
+    if (!c) return fail(KVR_E_INVAL, "NULL packed cache");
+    if (c->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned by an earlier CUDA error");
+    kvr_model *m = c->model;
+    KVR_TRY(check_range(m, positions, n_pos, l0, l1, c->cap));
+    for (int i = 0, end = c->n; i < n_pos; ++i) {
+      if (positions[i] > end)
+        return fail(KVR_E_RANGE, "position %d leaves a gap after %d", positions[i], end);
+      end = std::max(end, positions[i] + 1);
+    }
+    if (n_pos == 0 || l0 == l1) return KVR_OK;
+    KVR_TRY(use_device(m));
+    KVR_TRY(check_device_ptr(m, k, "k"));
+    KVR_TRY(check_device_ptr(m, v, "v"));
+    PackedRows rows;
+    KVR_TRY(rows_of(m, positions, n_pos, rows));
+    const int len = std::max(c->n, positions[n_pos - 1] + 1);
+    const int n =
+        launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->stream);
+    const kvr_status st = launched(m, n, "packed write");
+    if (st)
+      c->poisoned = true;
+    else
+      c->n = len;
+    return st;
+  });
 }
 
 kvr_status kvr_packed_read(const kvr_packed *c, const int32_t *positions, int32_t n_pos,
                            int32_t l0, int32_t l1, void *k_out, void *v_out) {
-  if (!c) return fail(KVR_E_INVAL, "NULL packed cache");
-  if (c->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned");
-  kvr_model *m = c->model;
-  KVR_TRY(check_range(m, positions, n_pos, l0, l1, c->n));
-  if (n_pos == 0 || l0 == l1) return KVR_OK;
-  KVR_TRY(use_device(m));
-  KVR_TRY(check_device_ptr(m, k_out, "k_out"));
-  KVR_TRY(check_device_ptr(m, v_out, "v_out"));
-  PackedRows rows;
-  KVR_TRY(rows_of(m, positions, n_pos, rows));
-  launch_packed_read(c->view(), m->dims.dtype, rows, l0, l1 - l0, k_out, v_out, m->stream);
-  return launched(m, 1, "packed read");
+  return guarded([&]() -> kvr_status {
+    if (!c) return fail(KVR_E_INVAL, "NULL packed cache");
+    if (c->poisoned) return fail(KVR_E_POISONED, "packed cache poisoned");
+    kvr_model *m = c->model;
+    KVR_TRY(check_range(m, positions, n_pos, l0, l1, c->n));
+    if (n_pos == 0 || l0 == l1) return KVR_OK;
+    KVR_TRY(use_device(m));
+    KVR_TRY(check_device_ptr(m, k_out, "k_out"));
+    KVR_TRY(check_device_ptr(m, v_out, "v_out"));
+    PackedRows rows;
+    KVR_TRY(rows_of(m, positions, n_pos, rows));
+    launch_packed_read(c->view(), m->dims.dtype, rows, l0, l1 - l0, k_out, v_out, m->stream);
+    return launched(m, 1, "packed read");
+  });
 }
 
 kvr_status kvr_packed_bounds(const kvr_packed *c, int32_t layer, int8_t *hi, int8_t *lo,
                              float *unit) {
-  if (!c || !hi || !lo || !unit) return fail(KVR_E_INVAL, "NULL argument");
-  kvr_model *m = c->model;
-  const Dims &dm = m->dims;
-  if (layer < 0 || layer >= dm.L) return fail(KVR_E_RANGE, "layer %d outside [0, %d)", layer, dm.L);
-  KVR_TRY(use_device(m));
-  KVR_TRY(synchronize(m));
-  const int used = (c->n + KVR_PAGE - 1) / KVR_PAGE;
-  const PackedView v = c->view();
-  std::vector<int8_t> both((size_t)used * 2 * dm.dh);
-  for (int g = 0; g < dm.G && used; ++g) {
-    const size_t at = v.index(layer, g, 0);
-    if (cudaMemcpy(both.data(), v.bounds + at * 2 * dm.dh, both.size(), cudaMemcpyDeviceToHost) !=
-            cudaSuccess ||
-        cudaMemcpy(unit + (size_t)g * used, v.unit + at, used * sizeof(float),
-                   cudaMemcpyDeviceToHost) != cudaSuccess)
-      return fail(KVR_E_CUDA, "bounds readback");
-    for (int b = 0; b < used; ++b) {
-      memcpy(hi + ((size_t)g * used + b) * dm.dh, both.data() + (size_t)b * 2 * dm.dh, dm.dh);
-      memcpy(lo + ((size_t)g * used + b) * dm.dh, both.data() + (size_t)(b * 2 + 1) * dm.dh, dm.dh);
+  return guarded([&]() -> kvr_status {
+    if (!c || !hi || !lo || !unit) return fail(KVR_E_INVAL, "NULL argument");
+    kvr_model *m = c->model;
+    const Dims &dm = m->dims;
+    if (layer < 0 || layer >= dm.L)
+      return fail(KVR_E_RANGE, "layer %d outside [0, %d)", layer, dm.L);
+    KVR_TRY(use_device(m));
+    KVR_TRY(synchronize(m));
+    const int used = (c->n + KVR_PAGE - 1) / KVR_PAGE;
+    const PackedView v = c->view();
+    std::vector<int8_t> both((size_t)used * 2 * dm.dh);
+    for (int g = 0; g < dm.G && used; ++g) {
+      const size_t at = v.index(layer, g, 0);
+      if (cudaMemcpy(both.data(), v.bounds + at * 2 * dm.dh, both.size(), cudaMemcpyDeviceToHost) !=
+              cudaSuccess ||
+          cudaMemcpy(unit + (size_t)g * used, v.unit + at, used * sizeof(float),
+                     cudaMemcpyDeviceToHost) != cudaSuccess)
+        return fail(KVR_E_CUDA, "bounds readback");
+      for (int b = 0; b < used; ++b) {
+        const int8_t *src = both.data() + (size_t)b * 2 * dm.dh;
+        memcpy(hi + ((size_t)g * used + b) * dm.dh, src, dm.dh);
+        memcpy(lo + ((size_t)g * used + b) * dm.dh, src + dm.dh, dm.dh);
+      }
     }
-  }
-  return KVR_OK;
+    return KVR_OK;
+  });
 }
 
 kvr_status kvr_rows_create(kvr_model *m, kvr_packed *const *docs, const int32_t *doc_rows,
                            int32_t n_docs, const int32_t *positions, kvr_rows **out) {
-  if (!m || !docs || !doc_rows || !positions || !out) return fail(KVR_E_INVAL, "NULL argument");
-  *out = nullptr;
-  if (n_docs < 1 || n_docs > MAX_DOCS)
-    return fail(KVR_E_RANGE, "n_docs=%d outside [1, %d]", n_docs, MAX_DOCS);
-  long long M = 0;
-  for (int d = 0; d < n_docs; ++d) {
-    if (!docs[d] || docs[d]->model != m) return fail(KVR_E_INVAL, "document %d: bad handle", d);
-    if (doc_rows[d] < 0) return fail(KVR_E_RANGE, "document %d: negative rows", d);
-    M += doc_rows[d];
-  }
-  if (M < 1 || M > MAX_ROWS) return fail(KVR_E_RANGE, "%lld rows outside [1, %d]", M, MAX_ROWS);
-  std::vector<kvr_packed *> dv(docs, docs + n_docs);
-  std::vector<int32_t> rv(doc_rows, doc_rows + n_docs);
-  KVR_TRY(check_rows(dv, rv, positions, (size_t)M));
-  KVR_TRY(use_device(m));
-  kvr_rows *r = new kvr_rows();
-  r->model = m;
-  r->docs = std::move(dv);
-  r->doc_rows = std::move(rv);
-  r->pos.resize(M);
-  m->rows.push_back(r);
-  if (const kvr_status st = build_rows(r, positions)) {
-    kvr_rows_free(r);
-    return st;
-  }
-  *out = r;
-  return KVR_OK;
+  kvr_rows *r = nullptr;
+  return guarded([&]() -> kvr_status {
+    if (!m || !docs || !doc_rows || !positions || !out) return fail(KVR_E_INVAL, "NULL argument");
+    *out = nullptr;
+    if (n_docs < 1 || n_docs > MAX_DOCS)
+      return fail(KVR_E_RANGE, "n_docs=%d outside [1, %d]", n_docs, MAX_DOCS);
+    long long M = 0;
+    for (int d = 0; d < n_docs; ++d) {
+      if (!docs[d] || docs[d]->model != m) return fail(KVR_E_INVAL, "document %d: bad handle", d);
+      if (doc_rows[d] < 0) return fail(KVR_E_RANGE, "document %d: negative rows", d);
+      M += doc_rows[d];
+    }
+    if (M < 1 || M > MAX_ROWS) return fail(KVR_E_RANGE, "%lld rows outside [1, %d]", M, MAX_ROWS);
+    std::vector<kvr_packed *> dv(docs, docs + n_docs);
+    std::vector<int32_t> rv(doc_rows, doc_rows + n_docs);
+    KVR_TRY(check_rows(dv, rv, positions, (size_t)M));
+    KVR_TRY(use_device(m));
+    r = new kvr_rows();
+    r->model = m;
+    m->rows.push_back(r);
+    r->docs = std::move(dv);
+    r->doc_rows = std::move(rv);
+    r->pos.resize(M);
+    if (const kvr_status st = build_rows(r, positions)) {
+      kvr_rows_free(r);
+      return st;
+    }
+    *out = r;
+    return KVR_OK;
+  }, [&] { kvr_rows_free(r); });
 }
 
 kvr_status kvr_rows_move(kvr_rows *r, const int32_t *positions) {
-  if (!r || !positions) return fail(KVR_E_INVAL, "NULL argument");
-  for (const kvr_packed *d : r->docs)
-    if (!d) return fail(KVR_E_INVAL, "a document of these rows has been freed");
-  KVR_TRY(check_rows(r->docs, r->doc_rows, positions, r->pos.size()));
-  KVR_TRY(use_device(r->model));
-  return build_rows(r, positions);
+  return guarded([&]() -> kvr_status {
+    if (!r || !positions) return fail(KVR_E_INVAL, "NULL argument");
+    for (const kvr_packed *d : r->docs)
+      if (!d) return fail(KVR_E_INVAL, "a document of these rows has been freed");
+    KVR_TRY(check_rows(r->docs, r->doc_rows, positions, r->pos.size()));
+    KVR_TRY(use_device(r->model));
+    return build_rows(r, positions);
+  });
 }
 
 void kvr_rows_free(kvr_rows *r) {
@@ -613,34 +640,40 @@ void kvr_rows_free(kvr_rows *r) {
 }
 
 kvr_status kvr_packed_attention(kvr_rows *r, int32_t layer, const void *q, int32_t ldq, void *out) {
-  PackedAttnArgs a;
-  KVR_TRY(rows_args(r, layer, q, ldq, a));
-  kvr_model *m = r->model;
-  KVR_TRY(check_device_ptr(m, out, "out"));
-  return attend_all(r, a, out);
+  return guarded([&]() -> kvr_status {
+    PackedAttnArgs a;
+    KVR_TRY(rows_args(r, layer, q, ldq, a));
+    kvr_model *m = r->model;
+    KVR_TRY(check_device_ptr(m, out, "out"));
+    return attend_all(r, a, out);
+  });
 }
 
 kvr_status kvr_packed_select(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
                              int32_t n_blocks, int32_t *blocks_out) {
-  PackedAttnArgs a;
-  KVR_TRY(rows_args(r, layer, q, ldq, a));
-  if (n_blocks < 1 || n_blocks > MAX_BLOCKS)
-    return fail(KVR_E_RANGE, "n_blocks=%d outside [1, %d]", n_blocks, MAX_BLOCKS);
-  kvr_model *m = r->model;
-  KVR_TRY(check_device_ptr(m, blocks_out, "blocks_out"));
-  return select_blocks(r, a, n_blocks, blocks_out);
+  return guarded([&]() -> kvr_status {
+    PackedAttnArgs a;
+    KVR_TRY(rows_args(r, layer, q, ldq, a));
+    if (n_blocks < 1 || n_blocks > MAX_BLOCKS)
+      return fail(KVR_E_RANGE, "n_blocks=%d outside [1, %d]", n_blocks, MAX_BLOCKS);
+    kvr_model *m = r->model;
+    KVR_TRY(check_device_ptr(m, blocks_out, "blocks_out"));
+    return select_blocks(r, a, n_blocks, blocks_out);
+  });
 }
 
 kvr_status kvr_packed_attention_blocks(kvr_rows *r, int32_t layer, const void *q, int32_t ldq,
                                        const int32_t *blocks, int32_t n_blocks, void *out) {
-  PackedAttnArgs a;
-  KVR_TRY(rows_args(r, layer, q, ldq, a));
-  if (n_blocks < 1 || n_blocks > MAX_BLOCKS)
-    return fail(KVR_E_RANGE, "n_blocks=%d outside [1, %d]", n_blocks, MAX_BLOCKS);
-  kvr_model *m = r->model;
-  KVR_TRY(check_device_ptr(m, out, "out"));
-  KVR_TRY(check_device_ptr(m, blocks, "blocks"));
-  return attend_blocks(r, a, blocks, n_blocks, out);
+  return guarded([&]() -> kvr_status {
+    PackedAttnArgs a;
+    KVR_TRY(rows_args(r, layer, q, ldq, a));
+    if (n_blocks < 1 || n_blocks > MAX_BLOCKS)
+      return fail(KVR_E_RANGE, "n_blocks=%d outside [1, %d]", n_blocks, MAX_BLOCKS);
+    kvr_model *m = r->model;
+    KVR_TRY(check_device_ptr(m, out, "out"));
+    KVR_TRY(check_device_ptr(m, blocks, "blocks"));
+    return attend_blocks(r, a, blocks, n_blocks, out);
+  });
 }
 
 }  // extern "C"

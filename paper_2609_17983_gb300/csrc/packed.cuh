@@ -32,6 +32,9 @@
 
 #include <cuda_fp16.h>
 
+#include <exception>
+#include <new>
+
 #include "kvr_internal.cuh"
 
 namespace kvr {
@@ -202,6 +205,27 @@ const char *launch_packed_attention(const PackedAttnArgs &a, cudaStream_t s);
 const char *launch_packed_select(const PackedAttnArgs &a, int max_pages, int32_t *blocks,
                                  cudaStream_t s);
 
+// An entry point's body: no C++ exception passes it (host memory that cannot be had is
+// KVR_E_NOMEM); `undo` runs after one.
+template <class F, class U>
+kvr_status guarded(F body, U undo) {
+  try {
+    return body();
+  } catch (const std::bad_alloc &) {
+    undo();
+    set_last_error("out of host memory");
+    return KVR_E_NOMEM;
+  } catch (const std::exception &e) {
+    undo();
+    set_last_error(e.what());
+    return KVR_E_INVAL;
+  }
+}
+template <class F>
+kvr_status guarded(F body) {
+  return guarded(body, [] {});
+}
+
 // ---- of api.cu, for the packed entry points ----
 // words of 32 bits to the device, ahead of what is queued next on the model's stream
 kvr_status upload_words(kvr_model *m, void *dst, const void *src, size_t words);
@@ -218,7 +242,8 @@ struct ManyPlan {
 bool many_plan(const kvr_model *m, const int32_t *pos, int rows, std::vector<int32_t> &tables,
                ManyPlan &p);
 kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, const void *q,
-                          int ldq, const int32_t *pos, void *pages, const int32_t *identity, void *out);
+                          int ldq, const int32_t *pos, void *pages, const int32_t *identity,
+                          void *out);
 // The first n_pages blocks of a layer as such pages, in halves.  A key row stored as NaN,
 // or whose value row is, becomes NaN; NaN value rows become zero.
 void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, bool settled,
@@ -254,6 +279,7 @@ struct kvr_rows {
   std::vector<kvr_packed *> docs;  // null: freed since
   std::vector<int32_t> doc_rows, pos;
   int n_parts = 0, n_tiles = 0, max_pages = 0, warps = 0, cluster = 0;
+  bool merged = false;   // some tile has more than one cluster
   bool sent = false;     // the device holds the tables of pos
   bool settled = false;  // and a kernel was launched behind their upload
   void *mem = nullptr;  // device tables
