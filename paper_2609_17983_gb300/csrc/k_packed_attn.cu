@@ -18,13 +18,14 @@
 // q is scaled by a power of two per vector so that it is a half as exactly as it
 // was a bf16; an fp32 model's q and P go as two halves each (22 bits), with
 // a page's products added to O in fp32 registers.  All sums are in fp32.
-// The warps' (max, sum, O) meet in shared memory, those of a cluster's CTAs in one
-// another's shared memory, each adding a slice; of several clusters the last to arrive
-// adds them all, in order.
+// The warps' (max, sum, O) meet in shared memory; those of a cluster's CTAs are brought
+// into the memory of the CTA that adds the slice (0.5 us sooner than read from there: a
+// token over 5000 positions 6.9 to 6.4); of several clusters the last to arrive adds
+// them all, in order.
 //
 // The floor is the cache's bytes: one token over 131072 positions of 8 KV heads reads 151 MB,
-// 22.3 us at the copy rate, and takes 31.5; sixteen documents of 8191 positions the same
-// in 31.1.  Of that about 5 us are the launch, the first copy's way and the sums; between
+// 22.3 us at the copy rate, and takes 31.1; sixteen documents of 8191 positions the same
+// in 30.7.  Of that about 5 us are the launch, the first copy's way and the sums; between
 // them an SM's 12 warps take 12 pages in 2.5 us, 6.7 TB/s over the chip, while its
 // schedulers issue half the time (1000 instructions a page and warp, 450 of them
 // conversions and byte permutations in the ALU's half-rate pipe).  mma.sync serves because
@@ -66,6 +67,14 @@ __device__ __forceinline__ void mma16816(float *d, const uint32_t *a, uint32_t b
       "{%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The cluster's barrier in two steps: what a thread wrote before its arrival, in whosever
+// memory, all see after their wait.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t r;
@@ -470,8 +479,12 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
         mbar_wait(&full[warp][i % STAGES][kv], i / STAGES & 1, abort_v, p.dev_flag, 0, false);
   __syncwarp();
 
-  // ---- the warps' sums ----
-  float *so = (float *)ring;  // [PACK_VEC][DH]
+  const int cl = p.cluster, rank = part % cl, nc = n_parts / cl;
+  if (cl > 1) cluster_arrive();  // this CTA is done with its copies' memory
+
+  // ---- the warps' sums, rows SD apart so that a column's four lanes meet four banks ----
+  constexpr int SD = DH + 4, D4 = DH / 4;
+  float *so = (float *)ring;  // [PACK_VEC][SD]
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
 #pragma unroll
@@ -479,35 +492,41 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     if (lg == 0) s_ml[warp][2 * lt + c] = make_float2(ref[c], l[c]);
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
-      so[(2 * lt + c) * DH + 16 * b + lg] = o[b][c];
-      so[(2 * lt + c) * DH + 16 * b + lg + 8] = o[b][c + 2];
+      so[(2 * lt + c) * SD + 16 * b + lg] = o[b][c];
+      so[(2 * lt + c) * SD + 16 * b + lg + 8] = o[b][c + 2];
     }
   }
   __syncthreads();
-  if (tid < PACK_VEC) {
-    float M = -INFINITY, L = 0.f;
+  if (tid < 16 * PACK_VEC) {  // sixteen lanes a vector, a lane a warp
+    const int vi = tid >> 4, w = tid & 15;
+    const float2 ml = w < WARPS ? s_ml[w][vi] : make_float2(-INFINITY, 0.f);
+    float M = ml.x;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) M = fmaxf(M, s_ml[w][tid].x);
+    for (int x = 8; x; x /= 2) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
+    const float f = merge_weight(ml.x, ml.y, M);
+    float L = f * ml.y;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      const float2 ml = s_ml[w][tid];
-      const float f = merge_weight(ml.x, ml.y, M);
-      s_wgt[w][tid] = f;
-      L += f * ml.y;
-    }
-    s_tot[tid] = make_float2(M, L);
+    for (int x = 8; x; x /= 2) L += __shfl_xor_sync(0xFFFFFFFFu, L, x);
+    if (w < WARPS) s_wgt[w][vi] = f;
+    if (w == 0) s_tot[vi] = make_float2(M, L);
   }
   __syncthreads();
-  auto out4 = [&](int i, float4 x, float L) {  // entries 4 (i % (DH / 4)) .. of the tile's vector
-    const int vec = vec0 + i / (DH / 4);
+  auto out4 = [&](int i, float4 x, float L) {  // entries 4 (i % D4) .. of the tile's vector i / D4
+    const int vec = vec0 + i / D4;
     const float f = L == 0.f ? 0.f : 1.f / L;  // no key: zeros
-    store4((T *)p.out + ((size_t)(vec / p.grp) * p.H + g * p.grp + vec % p.grp) * DH +
-               4 * (i % (DH / 4)),
+    store4((T *)p.out + ((size_t)(vec / p.grp) * p.H + g * p.grp + vec % p.grp) * DH + 4 * (i % D4),
            x.x * f, x.y * f, x.z * f, x.w * f);
   };
-  // ---- the cluster's sums: each CTA adds a slice of them, out of everyone's memory ----
-  const int cl = p.cluster, rank = part % cl, nc = n_parts / cl;
-  const int n4 = nvec * (DH / 4), per4 = (n4 + cl - 1) / cl;
+  auto warps_sum = [&](int i) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w)
+      add4(x, s_wgt[w][i / D4],
+           *(const float4 *)(smem + w * (STAGES * 2 * HB) + (i / D4 * SD + i % D4 * 4) * 4));
+    return x;
+  };
+  // ---- the cluster's sums: each CTA adds a slice of them, which the others bring ----
+  const int n4 = nvec * D4, per4 = (n4 + cl - 1) / cl;
   const int i0 = min(n4, rank * per4), i1 = min(n4, i0 + per4);
   const size_t slot0 = ((size_t)(slot / cl) * p.G + g), at = slot0 + (size_t)(part / cl) * p.G;
   auto finish = [&](int i, float4 x, float M, float L) {
@@ -515,50 +534,46 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
       out4(i, x, L);
       return;
     }
-    ((float4 *)p.ws_o)[at * PACK_VEC * (DH / 4) + i] = x;
-    if (i == i0 || i % (DH / 4) == 0)
-      p.ws_ml[(at * PACK_CLUSTER + rank) * PACK_VEC + i / (DH / 4)] = make_float2(M, L);
-  };
-  auto warps_sum = [&](int i) {
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w)
-      add4(x, s_wgt[w][i / (DH / 4)], ((const float4 *)(smem + w * (STAGES * 2 * HB)))[i]);
-    return x;
+    ((float4 *)p.ws_o)[at * PACK_VEC * D4 + i] = x;
+    if (i == i0 || i % D4 == 0)
+      p.ws_ml[(at * PACK_CLUSTER + rank) * PACK_VEC + i / D4] = make_float2(M, L);
   };
   if (cl == 1) {
     for (int i = tid; i < n4; i += WARPS * 32)
-      finish(i, warps_sum(i), s_tot[i / (DH / 4)].x, s_tot[i / (DH / 4)].y);
+      finish(i, warps_sum(i), s_tot[i / D4].x, s_tot[i / D4].y);
   } else {
     namespace cg = cooperative_groups;
     const cg::cluster_group cluster = cg::this_cluster();
-    float4 *sum = (float4 *)smem + PACK_VEC * (DH / 4);  // behind the first warp's sums
-    for (int i = tid; i < n4; i += WARPS * 32) sum[i] = warps_sum(i);
-    cluster.sync();
+    // behind the first warp's sums: [rank][per4] sums, [rank][PACK_VEC] (max, sum)
+    float4 *sums = (float4 *)(smem + 64 * DH);
+    float2 *mls = (float2 *)(smem + 112 * DH);
+    static_assert(PACK_VEC * SD * 4 <= 64 * DH &&
+                      64 * DH + (PACK_VEC * D4 + PACK_CLUSTER) * 16 <= 112 * DH &&
+                      112 * DH + PACK_CLUSTER * PACK_VEC * 8 <= STAGES * 2 * HB,
+                  "within a warp's ring");
+    cluster_wait();  // all are done with theirs
+    for (int i = tid; i < n4; i += WARPS * 32) {
+      const int to = i / per4;
+      cluster.map_shared_rank(sums, to)[rank * per4 + i - to * per4] = warps_sum(i);
+    }
+    for (int i = tid; i < cl * PACK_VEC; i += WARPS * 32)
+      cluster.map_shared_rank(mls, i / PACK_VEC)[rank * PACK_VEC + i % PACK_VEC] =
+          s_tot[i % PACK_VEC];
+    cluster_arrive();
+    cluster_wait();
     for (int i = i0 + tid; i < i1; i += WARPS * 32) {
-      const int vi = i / (DH / 4);
-      float2 ml[PACK_CLUSTER];
-      float4 y[PACK_CLUSTER];
+      const int vi = i / D4;
       float M = -INFINITY, L = 0.f;
-#pragma unroll
-      for (int k = 0; k < PACK_CLUSTER; ++k)
-        if (k < cl) {
-          ml[k] = *cluster.map_shared_rank(&s_tot[vi], k);
-          y[k] = *cluster.map_shared_rank(sum + i, k);
-          M = fmaxf(M, ml[k].x);
-        }
+      for (int k = 0; k < cl; ++k) M = fmaxf(M, mls[k * PACK_VEC + vi].x);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < PACK_CLUSTER; ++k)
-        if (k < cl) {
-          const float f = merge_weight(ml[k].x, ml[k].y, M);
-          L += f * ml[k].y;
-          add4(x, f, y[k]);
-        }
+      for (int k = 0; k < cl; ++k) {
+        const float2 ml = mls[k * PACK_VEC + vi];
+        const float f = merge_weight(ml.x, ml.y, M);
+        L += f * ml.y;
+        add4(x, f, sums[k * per4 + i - i0]);
+      }
       finish(i, x, M, L);
     }
-    // nobody leaves, or writes to its sums, while another reads them
-    cluster.sync();
   }
   if (nc == 1) return;
   __threadfence();
@@ -574,16 +589,16 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
   constexpr int MERGE = 20;
   float *wgt = (float *)smem;  // [nc][PACK_VEC]
   const size_t step = p.G;
-  const float4 *src = (const float4 *)p.ws_o + slot0 * PACK_VEC * (DH / 4);
+  const float4 *src = (const float4 *)p.ws_o + slot0 * PACK_VEC * D4;
   float4 y[MERGE];
   auto fetch_sums = [&](int i, int k0) {
 #pragma unroll
     for (int k = 0; k < MERGE; ++k)
-      if (k0 + k < nc) y[k] = __ldcg(src + i + (k0 + k) * step * PACK_VEC * (DH / 4));
+      if (k0 + k < nc) y[k] = __ldcg(src + i + (k0 + k) * step * PACK_VEC * D4);
   };
   if (i0 + tid < i1) fetch_sums(i0 + tid, 0);
   if (i0 < i1)
-    for (int vi = i0 / (DH / 4) + warp; vi <= (i1 - 1) / (DH / 4); vi += WARPS) {
+    for (int vi = i0 / D4 + warp; vi <= (i1 - 1) / D4; vi += WARPS) {
       const float2 *part_ml = p.ws_ml + (slot0 * PACK_CLUSTER + rank) * PACK_VEC + vi;
       float M = -INFINITY, L = 0.f;
       for (int k = lane; k < nc; k += 32)
@@ -602,7 +617,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     }
   __syncthreads();
   for (int i = i0 + tid; i < i1; i += WARPS * 32) {
-    const int vi = i / (DH / 4);
+    const int vi = i / D4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int k0 = 0; k0 < nc; k0 += MERGE) {
       if (k0 || i != i0 + tid) fetch_sums(i, k0);

@@ -134,14 +134,14 @@ struct Deal {
 };
 
 // The deal whose launch is modelled to end first, in units of 10 ns.  A wave of CTAs costs
-// 4.9 us beside its rounds (a page for each of a CTA's warps), a round 1.6 and 0.08 per
-// busy warp of the SM; a cluster's sums 1.3, a merge through memory 3.4 and 0.07 per
-// cluster; clusters of 4 and 8 leave 1/20 and 3/8 of the SMs without a place.  Fitted to
-// 6900 launches of 1 to 64 rows over 64 to 131072 positions: the deal taken is 0.9% slower
-// than the fastest on average, 15% at most.  One token over 5000 positions, 4 KV heads: 8
-// CTAs of 12 warps as a cluster 7.0 us (merged through memory 9.2, with 4 warps 8.6); over
-// 131072, 8 KV heads: 19 CTAs of 12 warps a head 32.4 (clusters of 4 34.2); 16 documents
-// of 8191: a CTA a document and head 32.4 (split in two 43.6).
+// 2.8 us beside its rounds (a page for each of a CTA's warps), a round 1.5; a cluster's
+// sums 1.4, a merge through memory 2.5 and 0.07 per cluster; clusters of 8 leave 7/20 of
+// the SMs without a place.  Fitted to 6900 launches of 1 to 64 rows over 64 to 131072
+// positions: the deal taken is 0.6% slower than the fastest on average, 14% at most.  One
+// token over 5000 positions, 4 KV heads: 8 CTAs of 12 warps as a cluster 6.6 us (merged
+// through memory 9.2, with 4 warps 7.6); over 131072, 8 KV heads: 19 CTAs of 12 warps a
+// head 31.3 (in clusters of 2 32.7); 16 documents of 8191: a CTA a document and head 31.3
+// (with 4 warps 34.2).
 Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int G) {
   const int many = m->dims.dtype == KVR_DTYPE_BF16 ? 12 : 8;
   int most = 1;
@@ -157,13 +157,12 @@ Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int
         long long ctas = 0;
         for (const auto &x : pages) ctas += (long long)d.parts(x.first) * x.second * G;
         const long long slots = std::max<long long>(
-            cl, (long long)m->num_sms * per_sm * (cl == 8 ? 25 : cl == 4 ? 38 : 40) / 40);
+            cl, (long long)m->num_sms * per_sm * (cl == 8 ? 13 : 20) / 20);
         const long long waves = (ctas + slots - 1) / slots;
-        const long long here = std::min<long long>(per_sm, (ctas + m->num_sms - 1) / m->num_sms);
         const int parts = d.parts(most), nc = parts / cl, each = (most + parts - 1) / parts;
-        const int deep = std::max(1, (each + W - 1) / W), busy = std::min(W, each);
-        const long long t = waves * (490 + deep * (160 + 8 * busy * here)) + (cl > 1 ? 130 : 0) +
-                            (nc > 1 ? 340 + 7 * nc : 0);
+        const int deep = std::max(1, (each + W - 1) / W);
+        const long long t =
+            waves * (280 + deep * 150) + (cl > 1 ? 140 : 0) + (nc > 1 ? 250 + 7 * nc : 0);
         if (least < 0 || t < least) least = t, best = d;
       }
       if (W * rounds >= most) break;
