@@ -753,9 +753,12 @@ __global__ void __launch_bounds__(2 * DH)
 // A cluster of CTAs per (row, KV head), each with a slice of the blocks: eight lanes a
 // block, SEL_AHEAD blocks of a lane in flight from the start (their loads cover those
 // of q).  The scores meet in the first CTA's shared memory, ordered as unsigned
-// numbers; it finds a threshold by bisection (which ends as soon as as many lie above as
-// are wanted) and writes the blocks in order, a warp a stretch of them.
+// numbers; it counts them into SEL_BINS bins of their range, then those of the bin that
+// holds the last one wanted into bins of its range, until a threshold parts as many as
+// are wanted (twice, as a rule; bisection took 14 rounds, 3 us of 6.8 for 1024 blocks);
+// and writes the blocks in order, a warp a stretch of them.
 constexpr int SEL_THREADS = 256, SEL_WARPS = SEL_THREADS / 32, SEL_AHEAD = 4;
+constexpr int SEL_BINS = 256, SEL_PASSES = 4;  // 8 bits of the 32 a pass
 template <int DH, typename T>
 __global__ void __launch_bounds__(SEL_THREADS)
     k_packed_select(const T *q, int ldq, const PackedRow *rows, int layer, int grp, int count,
@@ -766,6 +769,7 @@ __global__ void __launch_bounds__(SEL_THREADS)
   __shared__ float amax[DH / 32];
   __shared__ uint32_t range[2][SEL_WARPS];
   __shared__ int tot[2][SEL_WARPS];
+  __shared__ __align__(16) int bins[SEL_PASSES][SEL_BINS];
   namespace cg = cooperative_groups;
   const cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -779,6 +783,9 @@ __global__ void __launch_bounds__(SEL_THREADS)
     for (int i = tid; i < count && rank == 0; i += SEL_THREADS) out[i] = i <= own ? i : -1;
     return;
   }
+  if (cl > 1) cluster_arrive();  // this CTA runs
+  if (rank == 0)
+    for (int i = tid; i < SEL_PASSES * SEL_BINS; i += SEL_THREADS) (&bins[0][0])[i] = 0;
   const int per = (own + cl - 1) / cl, b0 = rank * per, b1 = min(own, b0 + per);
   const int sub = lane >> 3, piece = lane & 7;
   const size_t at = r.doc.index(layer, g, 0);
@@ -827,6 +834,7 @@ __global__ void __launch_bounds__(SEL_THREADS)
 #pragma unroll
   for (int i = 0; i < W; ++i) qv[i] = ((const int4 *)qs)[piece * W + i];
   uint32_t *all = cl > 1 ? cluster.map_shared_rank(keys, 0) : keys;
+  if (cl > 1) cluster_wait();  // so does the first, whose memory is written
   for (int b = first; b - sub - 4 * warp < b1; b += 4 * SEL_WARPS * SEL_AHEAD) {
     if (b != first) fetch(b);
 #pragma unroll
@@ -852,7 +860,8 @@ __global__ void __launch_bounds__(SEL_THREADS)
     }
   }
   if (cl > 1) {
-    cluster.sync();
+    cluster_arrive();
+    cluster_wait();
     if (rank) return;
   } else {
     __syncthreads();
@@ -867,19 +876,45 @@ __global__ void __launch_bounds__(SEL_THREADS)
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < SEL_WARPS; ++w) lo = min(lo, range[0][w]), hi = max(hi, range[1][w]);
-  // at least `want` are >= lo, fewer are > hi
-  for (int step = 0; lo < hi && want > 0; step ^= 1) {
-    const uint32_t mid = lo + (hi - lo + 1) / 2;
-    int n = 0;
-    for (int b = tid; b < own; b += SEL_THREADS) n += keys[b] >= mid;
-    n = __reduce_add_sync(0xFFFFFFFFu, n);
-    if (lane == 0) tot[step][warp] = n;
+  // `above` keys are > hi, fewer than wanted; with those in [lo, hi] it is as many at least
+  int above = 0;
+  for (int pass = 0; lo < hi && want > 0; ++pass) {
+    const int shift = max(0, 24 - __clz(hi - lo));  // the range's bits, but for eight
+    for (int b = tid; b < own; b += SEL_THREADS) {
+      const uint32_t x = keys[b];
+      if (x >= lo && x <= hi) atomicAdd(&bins[pass][(x - lo) >> shift], 1);
+    }
     __syncthreads();
-    n = 0;
+    // every warp: eight bins a lane, the highest first
+    int n[8], sum = 0;
+    *(int4 *)&n[0] = *(const int4 *)&bins[pass][SEL_BINS - 8 - 8 * lane];
+    *(int4 *)&n[4] = *(const int4 *)&bins[pass][SEL_BINS - 4 - 8 * lane];
 #pragma unroll
-    for (int w = 0; w < SEL_WARPS; ++w) n += tot[step][w];
-    if (n >= want) lo = mid;
-    if (n <= want) hi = n == want ? mid : mid - 1;
+    for (int i = 0; i < 8; ++i) sum += n[i];
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint32_t reach = __ballot_sync(0xFFFFFFFFu, above + upto >= want);
+    const int at_lane = __ffs(reach) - 1;
+    int before = above + upto - sum, bin = 0, held = 0;  // (those of lane at_lane count)
+    bool found = false;
+#pragma unroll
+    for (int i = 7; i >= 0; --i)
+      if (!found) {
+        if (before + n[i] >= want)
+          found = true, bin = SEL_BINS - 8 - 8 * lane + i, held = n[i];
+        else
+          before += n[i];
+      }
+    bin = __shfl_sync(0xFFFFFFFFu, bin, at_lane);
+    held = __shfl_sync(0xFFFFFFFFu, held, at_lane);
+    above = __shfl_sync(0xFFFFFFFFu, before, at_lane);
+    lo += (uint32_t)bin << shift;
+    // all of the bin, or some of it
+    hi = above + held == want ? lo : lo + min(hi - lo, (1u << shift) - 1);
   }
   const uint32_t t = lo;
   // keys above t, and as many of those equal to it as are wanted, in order
@@ -888,10 +923,10 @@ __global__ void __launch_bounds__(SEL_THREADS)
   for (int b = w0 + lane; b < w1; b += 32) gt += keys[b] > t, eq += keys[b] == t;
   gt = __reduce_add_sync(0xFFFFFFFFu, gt);
   eq = __reduce_add_sync(0xFFFFFFFFu, eq);
-  __syncthreads();
   if (lane == 0) tot[0][warp] = gt, tot[1][warp] = eq;
   __syncthreads();
-  int above = 0, gts = 0, eqs = 0;  // above t in all, and before this warp's stretch
+  int gts = 0, eqs = 0;  // before this warp's stretch
+  above = 0;
 #pragma unroll
   for (int w = 0; w < SEL_WARPS; ++w) {
     above += tot[0][w];
@@ -1024,10 +1059,15 @@ const char *select_blocks(const PackedAttnArgs &a, int max_pages, int32_t *block
   const size_t smem = (size_t)max_pages * sizeof(uint32_t);
   if (smem > 40 * 1024)
     if (const char *e = smem_opt_in(state, kernel, smem)) return e;
-  // a CTA for every 64 blocks of a row (its warps' loads are in flight at once for 128) as
-  // long as the chip takes them all together
+  // A CTA for every 128 blocks or more of a row, its warps' loads in flight at once, as long as
+  // the chip takes all of them together (four an SM); for fewer than 256 blocks a CTA where
+  // half the SMs would idle.  1024 blocks: 8 (row, KV head)s by 8 CTAs each 6.0 us (by one
+  // 11.3), 128 by 4 CTAs 10.6 (one 14.1, eight 14.1); 193 blocks: 8 by 2 4.5 (one 4.7), 128
+  // by one 6.1 (two 6.6).
   int cl = 1;
-  while (cl < 8 && max_pages > 64 * cl && (long long)a.n_rows * a.G * cl * 2 <= 2 * a.num_sms)
+  while (cl < 8 && max_pages > 128 * cl &&
+         (long long)a.n_rows * a.G * cl * 4 <=
+             (long long)a.num_sms * (max_pages >= 256 * cl ? 8 : 1))
     cl *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(a.n_rows * cl, a.G);

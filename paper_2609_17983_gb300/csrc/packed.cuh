@@ -87,6 +87,15 @@ struct PackedView {
   }
 };
 
+// The cluster's barrier in two steps: what a thread wrote before its arrival, in whosever
+// memory, all see after their wait.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+
 // The values of a word's eight codes, a half2 (low nibble first) for each byte.  Taken
 // apart into bytes by one mov, the conversions read them where they lie; extracted by
 // shifts each cost one more ALU instruction (15 clocks a word instead of 10.5).

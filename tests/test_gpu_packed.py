@@ -357,6 +357,30 @@ def test_selection_ties_and_queries_that_are_not_finite(models):
     r.close()
 
 
+@pytest.mark.parametrize("n", [3000, 20000])
+def test_selection_of_scores_far_apart(models, n):
+    """Scores of both signs over 30 binades, many of them equal, zeros among them."""
+    dh, H, G = SHAPES["dh64"]
+    m = models("dh64", "bf16")
+    rng = np.random.default_rng(n)
+    blocks = -(-n // 64)
+    factor = np.sign(rng.normal(size=blocks)) * np.exp2(rng.integers(-18, 12, blocks))
+    factor[rng.integers(0, blocks, blocks // 4)] = 0.0
+    one = rows(3, 64, 1, G, dh, "bf16")
+    x = torch.cat([one * float(f) for f in factor])[:n].expand(n, 2, G, dh).contiguous()
+    doc = m.packed(n)
+    doc.write(np.arange(n), x, x)
+    pos = [n // 2, n - 1]
+    r = m.rows([(doc, pos)])
+    q = queries(4, 2, H, dh, "bf16")
+    k = read(doc, np.arange(n), 2, G, dh, "bf16")[0][:, 0]
+    for count in (1, 2, 7, blocks // 3, blocks - 2):
+        got = torch.empty((2, G, count), dtype=torch.int32, device="cuda")
+        r.select(0, q, got)
+        assert np.array_equal(got.cpu().numpy(), pp.select(f64(q), np.array(pos), k, count))
+    r.close()
+
+
 def test_block_lists_of_the_caller(models):
     """Any order, entries outside the row's reach, none at all, long lists."""
     dh, H, G = SHAPES["dh128"]
