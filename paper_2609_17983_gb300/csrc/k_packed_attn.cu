@@ -119,6 +119,25 @@ __device__ __forceinline__ void scales(uint32_t w, uint32_t &a, uint32_t &b) {
   b = __byte_perm(w, 0, 0x4342) << 7;
 }
 
+// Scales as halves: whether any is NaN (their sum is, and only then: none is negative), and
+// those that are made zero (the larger of it and zero).
+__device__ __forceinline__ __half2 half2_in(uint32_t x) { return *(const __half2 *)&x; }
+__device__ __forceinline__ bool some_nan(uint4 x, uint4 y) {
+  const __half2 a = __hadd2(__hadd2(half2_in(x.x), half2_in(x.y)),
+                            __hadd2(half2_in(x.z), half2_in(x.w))),
+                b = __hadd2(__hadd2(half2_in(y.x), half2_in(y.y)),
+                            __hadd2(half2_in(y.z), half2_in(y.w))),
+                c = __hadd2(a, b);
+  return !__hbeq2(c, c);
+}
+__device__ __forceinline__ void no_nan(uint4 &x) {
+  auto f = [](uint32_t &u) {
+    const __half2 r = __hmax2(half2_in(u), __half2half2(__ushort_as_half(0)));
+    u = *(const uint32_t *)&r;
+  };
+  f(x.x), f(x.y), f(x.z), f(x.w);
+}
+
 // Four entries of a row of q.
 __device__ __forceinline__ void load4(const __nv_bfloat16 *p, float *x) {
   const uint2 u = *(const uint2 *)p;
@@ -298,6 +317,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
   for (; done < n_my; ++done) {
     const int st = done % STAGES;
     uint8_t *kb = ring + st * 2 * HB, *vb = kb + HB;
+    const int voff = (int)(vb - smem) + 16 * lane;  // (HB is whole 128s)
     bool ok = mbar_wait(&full[warp][st][0], done / STAGES & 1, abort_v, p.dev_flag, 1 << 12);
     if (!__all_sync(0xFFFFFFFFu, ok)) break;
     float s[4][4];
@@ -337,18 +357,21 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     if (!__all_sync(0xFFFFFFFFu, ok)) break;
     // scores; masked keys get none
     float top[2] = {-INFINITY, -INFINITY};
-    // V rows marked NaN (all their scales): any byte of the first entries' scales
-    uint32_t nan[4];
-    {
-      const uint4 n4 = *(const uint4 *)(vb + CB + lt * 16);
-      nan[0] = __vcmpeq4(n4.x, 0xFFFFFFFFu);
-      nan[1] = __vcmpeq4(n4.y, 0xFFFFFFFFu);
-      nan[2] = __vcmpeq4(n4.z, 0xFFFFFFFFu);
-      nan[3] = __vcmpeq4(n4.w, 0xFFFFFFFFu);
+    // V's scales as halves, once for the eight lanes that take each, where K was
+    uint4 *vs16 = (uint4 *)kb;  // [pairs of tiles 0 1, 2 3][db][t]
+    uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
+    if (lane < 4 * DB) {
+      const uint4 c4 = *(const uint4 *)(vb + CB + lane * 16);
+      scales(c4.x, x.x, x.y);
+      scales(c4.y, x.z, x.w);
+      scales(c4.z, y.x, y.y);
+      scales(c4.w, y.z, y.w);
     }
-    const bool any_nan = __any_sync(0xFFFFFFFFu, (nan[0] | nan[1] | nan[2] | nan[3]) != 0);
-    if (any_nan) {
-      // their scores become NaN, their scales zero
+    if (__any_sync(0xFFFFFFFFu, some_nan(x, y))) {
+      // rows marked NaN (all their scales): their scores become NaN, their scales zero
+      const uint4 n4 = *(const uint4 *)(vb + CB + lt * 16);
+      const uint32_t nan[4] = {__vcmpeq4(n4.x, 0xFFFFFFFFu), __vcmpeq4(n4.y, 0xFFFFFFFFu),
+                               __vcmpeq4(n4.z, 0xFFFFFFFFu), __vcmpeq4(n4.w, 0xFFFFFFFFu)};
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
         const uint32_t m = __shfl_sync(0xFFFFFFFFu, nan[kt], lg >> 1);  // keys 4 (lg / 2) .. + 3
@@ -356,21 +379,11 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
         for (int h = 0; h < 2; ++h)
           if (m >> (8 * ((lg & 1) + 2 * h)) & 1) s[kt][2 * h] = s[kt][2 * h + 1] = NAN;
       }
-      for (int i = lane; i < DB * 16; i += 32) {
-        uint32_t *x = (uint32_t *)(vb + CB) + i;
-        *x &= ~__vcmpeq4(*x, 0xFFFFFFFFu);
-      }
+      no_nan(x);
+      no_nan(y);
     }
     __syncwarp();
-    // V's scales as halves, once for the eight lanes that take each, where K was
-    uint4 *vs16 = (uint4 *)kb;  // [pairs of tiles 0 1, 2 3][db][t]
     if (lane < 4 * DB) {
-      const uint4 c4 = *(const uint4 *)(vb + CB + lane * 16);
-      uint4 x, y;
-      scales(c4.x, x.x, x.y);
-      scales(c4.y, x.z, x.w);
-      scales(c4.z, y.x, y.y);
-      scales(c4.w, y.z, y.w);
       vs16[lane] = x;
       vs16[4 * DB + lane] = y;
     }
@@ -438,7 +451,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     __syncwarp();
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
-      const uint4 w4 = *(const uint4 *)(vb + (b * 32 + (lane ^ b)) * 16);
+      const uint4 w4 = *(const uint4 *)(smem + (voff ^ 16 * b) + 512 * b);  // unit lane ^ b
       const uint4 x4 = vs16[b * 4 + lt], y4 = vs16[4 * DB + b * 4 + lt];
       const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
       const uint32_t vs[8] = {x4.x, x4.y, x4.z, x4.w, y4.x, y4.y, y4.z, y4.w};
