@@ -593,6 +593,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
   // flight a thread, the first of them while the weights are found (a warp a vector) ----
   constexpr int MERGE = 20;
   float *wgt = (float *)smem;  // [nc][PACK_VEC]
+  static_assert(PACK_MERGE * PACK_VEC * 4 <= WARPS * STAGES * 2 * HB, "within the rings");
   const size_t step = p.G;
   const float4 *src = (const float4 *)p.ws_o + slot0 * PACK_VEC * D4;
   float4 y[MERGE];

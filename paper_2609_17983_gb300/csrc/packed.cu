@@ -160,6 +160,7 @@ Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int
             cl, (long long)m->num_sms * per_sm * (cl == 8 ? 13 : 20) / 20);
         const long long waves = (ctas + slots - 1) / slots;
         const int parts = d.parts(most), nc = parts / cl, each = (most + parts - 1) / parts;
+        if (nc > PACK_MERGE) continue;
         const int deep = std::max(1, (each + W - 1) / W);
         const long long t =
             waves * (280 + deep * 150) + (cl > 1 ? 140 : 0) + (nc > 1 ? 250 + 7 * nc : 0);

@@ -172,6 +172,7 @@ void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, 
 // rows of one document; its pages are dealt to parts, a CTA each.
 constexpr int PACK_VEC = 8;
 constexpr int PACK_CLUSTER = 8;  // parts whose sums meet in shared memory, at most
+constexpr int PACK_MERGE = 1024;  // clusters of a tile: their weights lie in a CTA's memory
 struct PackedPart {
   const uint8_t *blocks;  // the document's
   int32_t pages;          // its capacity
