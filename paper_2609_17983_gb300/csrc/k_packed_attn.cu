@@ -24,8 +24,8 @@
 // them all, in order.
 //
 // The floor is the cache's bytes: one token over 131072 positions of 8 KV heads reads 151 MB,
-// 22.3 us at the copy rate, and takes 31.1; sixteen documents of 8191 positions the same
-// in 30.7.  Of that about 5 us are the launch, the first copy's way and the sums; between
+// 22.3 us at the copy rate, and takes 30.9; sixteen documents of 8191 positions the same
+// in 30.5.  Of that about 5 us are the launch, the first copy's way and the sums; between
 // them an SM's 12 warps take 12 pages in 2.5 us, 6.7 TB/s over the chip, while its
 // schedulers issue half the time (1000 instructions a page and warp, 450 of them
 // conversions and byte permutations in the ALU's half-rate pipe).  mma.sync serves because
