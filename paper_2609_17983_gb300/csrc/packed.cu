@@ -263,6 +263,7 @@ kvr_status build_rows(kvr_rows *r, const int32_t *pos) {
   memcpy(host.data() + o_many, tables.data(), tables.size() * 4);
   for (int i = 0; i < many_pages; ++i) ((int32_t *)(host.data() + o_id))[i] = i;
   r->sent = r->settled = false;
+  r->lists.n = 0;
   KVR_TRY(grow_device(m, r->mem, r->mem_bytes, bytes, "query rows"));
   KVR_TRY(upload_words(m, r->mem, host.data(), bytes / 4));
   char *base = (char *)r->mem;
@@ -401,8 +402,12 @@ kvr_status attend_blocks(kvr_rows *r, PackedAttnArgs &a, const int32_t *blocks, 
   const long long tiles = (long long)a.n_rows * ((a.grp + PACK_VEC - 1) / PACK_VEC);
   if (tiles * n_blocks > 0x7FFFFFFF)
     return fail(KVR_E_UNSUPPORTED, "too many rows (%d) for %d blocks each", a.n_rows, n_blocks);
-  Deal dl = deal(m, {{n_blocks, (int)tiles}}, a.G);
-  dl.per = std::min(dl.per, packed_attn_max_blocks_per_part());
+  auto &plan = r->lists;
+  if (plan.n != n_blocks) {
+    const Deal d = deal(m, {{n_blocks, (int)tiles}}, a.G);
+    plan = {n_blocks, d.warps, std::min(d.per, packed_attn_max_blocks_per_part()), d.cluster};
+  }
+  const Deal dl{plan.warps, plan.per, plan.cluster};
   a.warps = dl.warps;
   a.cluster = dl.cluster;
   a.parts_per_row = dl.parts(n_blocks);

@@ -289,6 +289,10 @@ struct kvr_rows {
   std::vector<kvr_packed *> docs;  // null: freed since
   std::vector<int32_t> doc_rows, pos;
   int n_parts = 0, n_tiles = 0, max_pages = 0, warps = 0, cluster = 0;
+  // how lists of n blocks are dealt (attend_blocks); n = 0: not yet
+  struct {
+    int n = 0, warps = 0, per = 0, cluster = 0;
+  } lists;
   bool merged = false;   // some tile has more than one cluster
   bool sent = false;     // the device holds the tables of pos
   bool settled = false;  // and a kernel was launched behind their upload

@@ -705,6 +705,7 @@ class Packed:
         self.h = handle
         c = model.cfg
         self._row = c["n_kv_heads"] * c["head_dim"]
+        self._layers = c["n_layers"]
         self._dtype = _torch_dtype(c)
         model._caches.add(self)
 
@@ -721,20 +722,20 @@ class Packed:
     def n(self) -> int:
         return kvr_packed_len(self.h)
 
-    def _rows(self, positions, layer_begin, layer_end, k, v):
+    def _call(self, f, positions, layer_begin, layer_end, k, v):
         ps = _i32(positions)
-        le = self.model.cfg["n_layers"] if layer_end is None else layer_end
-        count = ps.size * max(le - layer_begin, 0) * self._row
-        return (ps, layer_begin, le, _device(k, "k", self._dtype, count),
-                _device(v, "v", self._dtype, count))
+        n, le = ps.size, self._layers if layer_end is None else layer_end
+        count = n * max(le - layer_begin, 0) * self._row
+        _check(f(self.h, ps.tobytes(), n, layer_begin, le, _device(k, "k", self._dtype, count),
+                 _device(v, "v", self._dtype, count)))
 
     def write(self, positions, k, v, layer_begin: int = 0, layer_end: int | None = None):
         """Quantise k and v into the cache at `positions` (kvr_packed_write)."""
-        kvr_packed_write(self.h, *self._rows(positions, layer_begin, layer_end, k, v))
+        self._call(_lib.kvr_packed_write, positions, layer_begin, layer_end, k, v)
 
     def read(self, positions, k_out, v_out, layer_begin: int = 0, layer_end: int | None = None):
         """The stored rows into k_out and v_out (kvr_packed_read)."""
-        kvr_packed_read(self.h, *self._rows(positions, layer_begin, layer_end, k_out, v_out))
+        self._call(_lib.kvr_packed_read, positions, layer_begin, layer_end, k_out, v_out)
 
     def repair(self, new_tokens, edit_start: int, positions):
         """Repair the packed document in place (kvr_packed_repair)."""
@@ -798,17 +799,17 @@ class Rows:
         qp, ldq = self._q(q)
         op = _device(out, "out", self._dtype, self.n * self._row)
         if blocks is None:
-            kvr_packed_attention(self.h, layer, qp, ldq, op)
+            _check(_lib.kvr_packed_attention(self.h, layer, qp, ldq, op))
             return
-        nb = blocks.shape[-1]
-        kvr_packed_attention_blocks(self.h, layer, qp, ldq,
-                                    _device(blocks, "blocks", self._int, self._lists * nb), nb,
-                                    op)
+        nb = blocks.size(-1)
+        _check(_lib.kvr_packed_attention_blocks(
+            self.h, layer, qp, ldq, _device(blocks, "blocks", self._int, self._lists * nb), nb, op))
 
     def select(self, layer: int, q, blocks_out):
         """The blocks that each row attends to (kvr_packed_select) into blocks_out, int32
         [rows][n_kv_heads][n_blocks]."""
         qp, ldq = self._q(q)
-        nb = blocks_out.shape[-1]
-        kvr_packed_select(self.h, layer, qp, ldq, nb,
-                          _device(blocks_out, "blocks_out", self._int, self._lists * nb))
+        nb = blocks_out.size(-1)
+        _check(_lib.kvr_packed_select(
+            self.h, layer, qp, ldq, nb,
+            _device(blocks_out, "blocks_out", self._int, self._lists * nb)))
