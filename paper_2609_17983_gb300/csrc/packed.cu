@@ -174,11 +174,12 @@ Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int
 
 // Whether the rows of a document at `pos` (ascending, >= 0) go by way of unpacked pages: one
 // kernel widens the layer's blocks to pages of halves, and the tcgen05 attention takes a tile of
-// 128 vectors at a time where the fused kernel takes 8.  By (page, tile of 8 vectors, KV
-// head) units u and positions n the fused kernel takes about 6 + 0.0015 u us (head size
-// 64: 4 + 0.0009 u), the other way 13 + 0.0008 n + 0.00025 u, for every document anew.  40
-// rows over 5000 positions (28 heads) 18 against 20 us, 64 rows 25 against 23; a chunk
-// of 4096 rows over 12345 positions 2993 against 478.
+// 128 vectors at a time where the fused kernel takes 8.  Units are (page, tile of 8 vectors,
+// KV head); where the other way is shorter was fitted to 270 launches by both, of 8 to 4096 rows
+// over 512 to 12345 positions: the one taken is 0.2% slower than the other on average,
+// 17% at most.  40 rows spread over 5000 positions (28 heads) 17.3 us against 20.4, the
+// last 64 27.7 against 23.0; a chunk of 4096 rows over 12345 positions 2794 against 474.  A
+// second document is unpacked anew.
 bool many_rows(const kvr_model *m, const int32_t *pos, int rows, size_t docs) {
   const Dims &dm = m->dims;
   if (dm.dtype != KVR_DTYPE_BF16 || rows < 1) return false;
@@ -187,7 +188,7 @@ bool many_rows(const kvr_model *m, const int32_t *pos, int rows, size_t docs) {
   for (int v = 0; v < rows * grp; v += PACK_VEC)
     units += pos[std::min(rows * grp - 1, v + PACK_VEC - 1) / grp] / KVR_PAGE + 1;
   const long long n = pos[rows - 1] + 1;
-  const long long least = dm.dh == 128 ? 5600 + n * 16 / 25 : 6500 + n * 9 / 10;
+  const long long least = dm.dh == 128 ? 6600 + n * 2 / 5 : 5000 + n * 26 / 25;
   return units * dm.G > least + (docs > 1 ? 5000 : 0);
 }
 
