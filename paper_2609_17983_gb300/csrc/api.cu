@@ -446,7 +446,8 @@ kvr_status rope(kvr_model *m, const Rows &r, int l, bool write_kv, const SplitVi
     KVR_TRY(launch_check(m, 1));
     const char *k = (const char *)m->rows_scratch;
     const int n = launch_packed_write(r.packed->view(), dm.dtype, r.packed_pos, r.packed_len, l, 1,
-                                      k, k + (size_t)r.M * dm.G * dm.dh * dm.es(), m->stream);
+                                      k, k + (size_t)r.M * dm.G * dm.dh * dm.es(), m->num_sms,
+                                      m->stream);
     return launch_check(m, n);
   }
   launch_rope_scatter(m->qkv, m->rope, r.pos, r.M, dm, l, r.views, r.rowdoc, r.single,
@@ -1839,7 +1840,8 @@ kvr_status kvr_pack(const kvr_cache *c, kvr_packed **out) {
       st = launch_check(m, 1);
       if (st) break;
       const int n =
-          launch_packed_write(p->view(), dm.dtype, rows, c->n, l, l1 - l, k, v, m->stream);
+          launch_packed_write(p->view(), dm.dtype, rows, c->n, l, l1 - l, k, v, m->num_sms,
+                              m->stream);
       st = launch_check(m, n);
     }
     if (st) {

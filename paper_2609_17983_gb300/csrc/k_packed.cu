@@ -147,18 +147,21 @@ struct Eight<float> {
   }
 };
 
-// Scale codes of n rows' groups, as this thread's eight entries and its neighbour's (lane
-// ^ 1) make them up; rows with a NaN or an infinity anywhere (rowmask: the lanes of a
-// row) get PACK_NAN.
+// Scale code of a row's group, as this thread's eight entries and its neighbour's (lane ^ 1)
+// make it up; rows with a NaN or an infinity anywhere (rowmask: the lanes of a row) get
+// PACK_NAN.
+template <typename T>
+__device__ __forceinline__ uint32_t scale_code(const Eight<T> &x, uint32_t rowmask) {
+  uint32_t m = x.magnitude();
+  const bool bad = (__ballot_sync(0xFFFFFFFFu, m >= 0x7F800000u) & rowmask) != 0;
+  m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+  return bad ? PACK_NAN : Eight<T>::scale_code(__uint_as_float(m));
+}
+// Those of N rows.
 template <int N>
 __device__ __forceinline__ void scale_codes(const Eight<float> *x, uint32_t rowmask, uint32_t *sc) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    uint32_t m = x[j].magnitude();
-    const bool bad = (__ballot_sync(0xFFFFFFFFu, m >= 0x7F800000u) & rowmask) != 0;
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-    sc[j] = bad ? PACK_NAN : pack_scale_code(__uint_as_float(m));
-  }
+  for (int j = 0; j < N; ++j) sc[j] = scale_code(x[j], rowmask);
 }
 // Two bf16 rows at a time: their magnitudes, halves of the sixths and codes in the 16-bit
 // halves of one register each (see pack_scale_code_bf16).
@@ -453,11 +456,14 @@ __global__ void __launch_bounds__(DH / 2)
 // quantised, K and V side by side in a warp, into shared memory, while the block's K
 // codes are on their way to registers and so are the V codes of the first groups of four
 // keys that change; words with a new key are patched and stored, and the bounds taken
-// over all rows present.  NT: DH / 2 threads for up to PATCH_FEW rows a page (the bounds'
-// warps alone, whose registers then hold all they need), 2 DH for more.  28 layers, 4 KV
-// heads: 40 rows of 40 pages 11.9 us (by 2 DH threads 25), 320 of 40 pages 16.5 (31), 480 of
-// 15 pages 21.3 (22.6), of 10 pages 26.9 (22.1).  which: the segments of a run that are not
-// whole pages (a list's are blockIdx.y).
+// over all rows present.  NT: 2 DH threads, of which a group's V takes DH / 8, who turn four
+// rows' codes at once; or DH / 2 (the bounds' warps alone, whose registers then hold all
+// they need), which take the rows one after another but four times as many blocks at once.
+// few_rows chooses; 28 layers, 4 KV heads, us by DH / 2 and by 2 DH threads:
+//   pages               3 rows of 1   3 of 10   12 of 10   12 of 40   32 of 10
+//   DH / 2 | 2 DH         4.5 | 3.9   7.4 | 8.5   13.9 | 11.2   27.8 | 36.2   23.4 | 13.5
+// (a row of each of 40 pages 11.7 | 25.3).  which: the segments of a run that are not whole
+// pages (a list's are blockIdx.y).
 constexpr int PATCH_FEW = 32;
 template <int DH, typename T, class Rows, int NT>
 __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
@@ -468,11 +474,12 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
                 KPT = 2 * DH / NT;  // 16-byte pieces of K a thread
   constexpr bool FEW = KPT == 4;
   constexpr int ROWS = FEW ? PATCH_FEW : KVR_PAGE;  // rows in shared memory
-  constexpr int VG = NT / (DH / 2);  // groups of V at a time, a word (entries i, i + 8) a thread
+  // groups of V at a time, and a thread's words of each: entries vi .. and the eighth past each
+  constexpr int VG = FEW ? 1 : NT / CH, VW = FEW ? 1 : 4;
   __shared__ float amax[2];
   __shared__ __align__(16) uint32_t code[ROWS][2][CH];
   __shared__ __align__(8) uint8_t scale[ROWS][2][DB];
-  __shared__ uint8_t row_at[KVR_PAGE];  // of a slot that is written
+  __shared__ __align__(4) uint8_t row_at[KVR_PAGE];  // of a slot that is written
   __shared__ __align__(16) uint8_t kbuf[FEW ? 16 : HB];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lg = lane >> 2, lt = lane & 3;
   const int g = blockIdx.x, l = blockIdx.z;
@@ -512,45 +519,49 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
   }
   const unsigned long long mask = __reduce_or_sync(0xFFFFFFFFu, mlo) |
                                   (unsigned long long)__reduce_or_sync(0xFFFFFFFFu, mhi) << 32;
-  // V: a thread's word of every VG-th of the groups of four keys that change
-  const int vdb = tid % (DH / 2) >> 3, vi = tid & 7;
-  auto next_group = [](unsigned long long &m) {  // the first group of four slots in m, and past it
-    if (!m) return -1;
-    const int kg = (__ffsll((long long)m) - 1) / 4;
-    m &= ~(15ull << (4 * kg));
-    return kg;
+  // V: the groups of four slots that change; threads of vi = 0 take the scales of their db too
+  const int vch = tid % CH, vdb = FEW ? tid >> 3 : vch >> 1, vi = FEW ? tid & 7 : 4 * (vch & 1);
+  uint32_t mine = __ballot_sync(0xFFFFFFFFu, lane < 16 && (mask >> (4 * (lane & 15)) & 15));
+  const int n_groups = __popc(mine);
+  if (!FEW)
+    for (int i = 0; i < tid / CH; ++i) mine &= mine - 1;
+  int kg;
+  uint32_t old[VW], old_s;
+  auto v_word = [&](int i) { return (uint32_t *)(vb + pack_v_code(kg, 16 * vdb + vi + i)); };
+  auto v_scales = [&]() { return (uint32_t *)(vb + pack_v_scale(DH, 4 * kg, vdb)); };
+  auto v_load = [&]() {  // what the thread's next group holds
+    kg = __ffs(mine) - 1;
+    if (kg < 0) return;
+#pragma unroll
+    for (int i = 0; i < VW; ++i) old[i] = *v_word(i);
+    if (vi == 0) old_s = *v_scales();
   };
-  unsigned long long mine = mask;
-  for (int i = 0; i < tid / (DH / 2); ++i) next_group(mine);
-  int kg = next_group(mine);
-  auto v_word = [&]() { return (uint32_t *)(vb + pack_v_code(kg, 16 * vdb + vi)); };
-  uint32_t old = kg >= 0 ? *v_word() : 0;
+  v_load();
   // the new rows, up to PRE of a warp's in flight
   {
     const int sub = lane / CH, ch = lane % CH;  // rows' halves side by side: K, V (twice for 64)
     const uint32_t rowmask = (CH == 16 ? 0xFFFFu : 0xFFu) << (lane & ~(CH - 1));
     constexpr int RPW = 32 / (2 * CH), PRE = FEW ? 2 : 4;  // rows of a warp at a time
     for (int i0 = warp * RPW; i0 < count; i0 += WARPS * RPW * PRE) {
-      Eight<T> x[PRE];
+      Eight<T> x[PRE];  // (past the last row: that one again)
+      uint32_t sc[PRE];
 #pragma unroll
       for (int j = 0; j < PRE; ++j) {
-        const int i = i0 + j * WARPS * RPW + sub / 2;
-        x[j] = Eight<T>{};
-        if (i < count)
-          x[j].load((sub & 1 ? val : k) + (((size_t)(sg.r0 + i) * gridDim.z + l) * v.G + g) * DH +
-                    8 * ch);
+        if (FEW && i0 + j * WARPS * RPW >= count) break;
+        const int i = min(i0 + j * WARPS * RPW + sub / 2, count - 1);
+        x[j].load((sub & 1 ? val : k) + (((size_t)(sg.r0 + i) * gridDim.z + l) * v.G + g) * DH +
+                  8 * ch);
       }
+      if (!FEW) scale_codes<PRE>(x, rowmask, sc);
 #pragma unroll
       for (int j = 0; j < PRE; ++j) {
         const int i = i0 + j * WARPS * RPW + sub / 2;
         if (i0 + j * WARPS * RPW >= count) break;
-        uint32_t m = x[j].magnitude();
-        const bool bad = (__ballot_sync(0xFFFFFFFFu, m >= 0x7F800000u) & rowmask) != 0;
-        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+        if (FEW) sc[j] = scale_code(x[j], rowmask);
         if (i < count) {
-          const uint32_t s = bad ? PACK_NAN : Eight<T>::scale_code(__uint_as_float(m));
-          code[i][sub & 1][ch] = bad || s == 0 ? 0 : x[j].codes(pack_scale(s));
-          if (!(ch & 1)) scale[i][sub & 1][ch >> 1] = (uint8_t)s;
+          code[i][sub & 1][ch] =
+              sc[j] == 0 || sc[j] == PACK_NAN ? 0 : x[j].codes(pack_scale(sc[j]));
+          if (!(ch & 1)) scale[i][sub & 1][ch >> 1] = (uint8_t)sc[j];
         }
         __syncwarp();
       }
@@ -585,22 +596,49 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 ? 1024 : 768) / NT)
           *(uint32_t *)(kbuf + CB + ((kt_of(i) * 8 + lg) * 2 + h) * DB + 4 * d4) = sc[i][h];
     }
   }
-  // V: the words of a group
-  while (kg >= 0) {
+  // V: the words of the groups
+  for (int n = 0; n < n_groups; n += VG) {
+    const uint32_t in = kg < 0 ? 0 : (uint32_t)(mask >> (4 * kg)) & 15;  // slots that are written
+    const uint32_t r4 = kg < 0 ? 0 : *(const uint32_t *)&row_at[4 * kg];
+    uint32_t w[VW] = {}, c[4], sn = 0, bytes = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (mask >> (4 * kg + j) & 1) {
-        const uint32_t *c = code[row_at[4 * kg + j]][1] + 2 * vdb;
-        const uint32_t n = (c[0] >> (4 * vi) & 15u) | (c[1] >> (4 * vi) & 15u) << 16;
-        old = (old & ~(0x000F000Fu << (4 * j))) | n << (4 * j);
+    for (int j = 0; j < 4; ++j) {
+      c[j] = 0;
+      if (in >> j & 1) {
+        const int r = r4 >> (8 * j) & 0xFF;
+        if (FEW) {
+          const uint32_t *x = code[r][1] + 2 * vdb;
+          w[0] |= ((x[0] >> (4 * vi) & 15u) | (x[1] >> (4 * vi) & 15u) << 16) << (4 * j);
+        } else {
+          c[j] = code[r][1][vch];
+        }
+        sn |= (uint32_t)scale[r][1][vdb] << (8 * j);
+        bytes |= 0xFFu << (8 * j);
       }
-    *v_word() = old;
-    for (int i = 1; i < VG; ++i) next_group(mine);  // the others'
-    kg = next_group(mine);
-    if (kg >= 0) old = *v_word();
+    }
+    if constexpr (!FEW) {
+      uint32_t h[4];
+      transpose_out(c, h);
+      // half-words of entries 0 2, 1 3 (of those past them: 4 6, 5 7) against the neighbour's
+      const uint32_t k0 = vi ? h[1] : h[0], k1 = vi ? h[3] : h[2],
+                     g0 = __shfl_xor_sync(0xFFFFFFFFu, vi ? h[0] : h[1], 1),
+                     g1 = __shfl_xor_sync(0xFFFFFFFFu, vi ? h[2] : h[3], 1);
+      const uint32_t lo[2] = {vi ? g0 : k0, vi ? g1 : k1}, hi[2] = {vi ? k0 : g0, vi ? k1 : g1};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = __byte_perm(lo[i & 1], hi[i & 1], i & 2 ? 0x7632 : 0x5410);
+    }
+    if (kg >= 0) {
+      uint32_t nibbles = (__byte_perm(bytes, 0, 0x4420) & 0x0F0Fu) |
+                         (__byte_perm(bytes, 0, 0x4431) & 0xF0F0u);
+      nibbles |= nibbles << 16;
+#pragma unroll
+      for (int i = 0; i < VW; ++i) *v_word(i) = (old[i] & ~nibbles) | w[i];
+      if (vi == 0) *v_scales() = (old_s & ~bytes) | sn;
+    }
+    for (int i = 0; i < VG; ++i) mine &= mine - 1;
+    v_load();
   }
-  for (int i = tid; i < count * DB; i += NT)
-    vb[pack_v_scale(DH, slot_of(i / DB), i % DB)] = scale[i / DB][1][i % DB];
   const size_t at = v.index(l0 + l, g, sg.page);
   if constexpr (FEW) {
     block_bounds<DH>(amax, w, sc, present, v.bounds + at * 2 * DH, v.unit + at);
@@ -949,10 +987,19 @@ __global__ void __launch_bounds__(SEL_THREADS)
 }  // namespace
 
 namespace {
+// Whether DH / 2 threads take a page's rows (most of them on a page, blocks in all): as long
+// as the rows past the first are at most 1.6 w^2, with w waves of CTAs of 2 DH threads.
+// Over 150 launches of 1 to 32 rows on each of 1 to 40 pages the kernel taken is 0.1% slower
+// than the other on average, 5% at most.
+template <int DH, typename T>
+bool few_rows(int most, long long blocks, int sms) {
+  const long long places = (long long)sms * ((sizeof(T) == 2 ? 1024 : 768) / (2 * DH));
+  return most <= PATCH_FEW && 5 * (most - 1) * places * places <= 8 * blocks * blocks;
+}
 // Pages that a run writes whole by k_packed_write_pages, all others by k_packed_patch.
 template <int DH, typename T, class Rows>
 int write_rows(const PackedView &v, const Rows &rows, int len, int l0, int nl, const void *k,
-               const void *val, cudaStream_t s) {
+               const void *val, int sms, cudaStream_t s) {
   int2 part{0, 0};
   int parts = rows.n_seg, launches = 0, most = rows.most;
   if (rows.first >= 0) {
@@ -976,7 +1023,7 @@ int write_rows(const PackedView &v, const Rows &rows, int len, int l0, int nl, c
       launch_pdl(kernel, dim3(v.G, parts, nl), dim3(threads), 0, s, v, rows, part, len, l0,
                  (const T *)k, (const T *)val);
     };
-    if (most <= PATCH_FEW)
+    if (few_rows<DH, T>(most, (long long)v.G * parts * nl, sms))
       patch(k_packed_patch<DH, T, Rows, DH / 2>, DH / 2);
     else
       patch(k_packed_patch<DH, T, Rows, 2 * DH>, 2 * DH);
@@ -1020,10 +1067,10 @@ void by_kind(int dh, int dtype, const PackedRows &rows, F f) {
 }  // namespace
 
 int launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows, int len, int l0,
-                        int nl, const void *k, const void *val, cudaStream_t s) {
+                        int nl, const void *k, const void *val, int sms, cudaStream_t s) {
   int launches = 0;
   by_kind(v.dh, dtype, rows, [&](auto d, auto t, const auto &r) {
-    launches = write_rows<decltype(d)::value, decltype(t)>(v, r, len, l0, nl, k, val, s);
+    launches = write_rows<decltype(d)::value, decltype(t)>(v, r, len, l0, nl, k, val, sms, s);
   });
   return launches;
 }

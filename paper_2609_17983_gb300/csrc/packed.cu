@@ -530,7 +530,8 @@ kvr_status kvr_packed_write(kvr_packed *c, const int32_t *positions, int32_t n_p
     KVR_TRY(rows_of(m, positions, n_pos, rows));
     const int len = std::max(c->n, positions[n_pos - 1] + 1);
     const int n =
-        launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->stream);
+        launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->num_sms,
+                            m->stream);
     const kvr_status st = launched(m, n, "packed write");
     if (st)
       c->poisoned = true;

@@ -164,7 +164,7 @@ struct PackedRows {
 // k, v: [n][nl][G][dh] in the model dtype; len: the document's length after the write.
 // Returns the kernels launched.
 int launch_packed_write(const PackedView &v, int dtype, const PackedRows &rows, int len, int l0,
-                        int nl, const void *k, const void *val, cudaStream_t s);
+                        int nl, const void *k, const void *val, int sms, cudaStream_t s);
 void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, int l0, int nl,
                         void *k, void *val, cudaStream_t s);
 

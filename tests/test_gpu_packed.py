@@ -129,6 +129,36 @@ def test_store_edges_of_the_grids(models, dtype):
     doc.close()
 
 
+@pytest.mark.parametrize("shape,dtype,pages,most", [
+    ("dh128", "bf16", 300, 6), ("dh64", "bf16", 420, 3), ("dh64", "fp32", 400, 3)])
+def test_store_some_rows_of_pages(models, shape, dtype, pages, most):
+    """A few rows of each of more blocks than the chip takes at once, then many rows of three
+    pages: next to one another or not, with a NaN and an infinity among them."""
+    dh, H, G = SHAPES[shape]
+    m = models(shape, dtype)
+    n = 64 * pages - 7
+    k, v = rows(1, n, 2, G, dh, dtype), rows(2, n, 2, G, dh, dtype)
+    doc = m.packed(n)
+    doc.write(np.arange(n), k, v)
+    rng = np.random.default_rng(pages)
+    few = [64 * p + rng.permutation(57)[:rng.integers(0 if p else most, most + 1)]
+           for p in range(pages)]
+    many = [64 * p + rng.permutation(57)[:41] for p in (0, 5, pages - 1)]
+    for at in (few, many):
+        at = np.sort(np.concatenate(at))
+        k2, v2 = rows(3, len(at), 2, G, dh, dtype), rows(4, len(at), 2, G, dh, dtype)
+        k2[len(at) // 2, 1, G - 1, 3], v2[len(at) // 3, 0, 0, dh - 1] = float("nan"), float("inf")
+        doc.write(at, k2, v2)
+        where = torch.from_numpy(at).cuda()
+        k[where], v[where] = k2, v2
+    want = pp.stored(f64(k)), pp.stored(f64(v))
+    got = read(doc, np.arange(n), 2, G, dh, dtype)
+    assert same(got[0], want[0]) and same(got[1], want[1])
+    for l in range(2):
+        assert all(same(a, b) for a, b in zip(doc.bounds(l), pp.bounds(want[0][:, l])))
+    doc.close()
+
+
 def test_store_many_scattered_rows(models):
     """More scattered positions than come with a launch."""
     dh, H, G = SHAPES["dh64"]
