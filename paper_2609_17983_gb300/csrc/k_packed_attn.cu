@@ -24,7 +24,7 @@
 // them all, in order.
 //
 // The floor is the cache's bytes: one token over 131072 positions of 8 KV heads reads 151 MB,
-// 22.3 us at the copy rate, and takes 30.9; sixteen documents of 8191 positions the same
+// 22.3 us at the copy rate, and takes 30.5; sixteen documents of 8191 positions the same
 // in 30.5.  Of that about 5 us are the launch, the first copy's way and the sums; between
 // them an SM's 12 warps take 12 pages in 2.5 us, 6.7 TB/s over the chip, while its
 // schedulers issue half the time (1000 instructions a page and warp, 450 of them
@@ -581,57 +581,80 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     }
   }
   if (nc == 1) return;
-  __threadfence();
+  // one thread's arrival releases, after the barrier, what all of the CTA wrote, and acquires
+  // what the others did
   __syncthreads();
   int *arrived = p.counters + ((size_t)counter * p.G + g) * PACK_CLUSTER + rank;
-  if (tid == 0) s_last = atomicAdd(arrived, 1) == nc - 1;
+  if (tid == 0) {
+    int before;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;"
+                 : "=r"(before)
+                 : "l"(arrived)
+                 : "memory");
+    s_last = before == nc - 1;
+  }
   __syncthreads();
   if (!s_last) return;
-  __threadfence();
   if (tid == 0) *arrived = 0;
   // ---- the last cluster's CTAs add the slices of all, in order: MERGE clusters' sums in
-  // flight a thread, the first of them while the weights are found (a warp a vector) ----
-  constexpr int MERGE = 20;
+  // flight a thread, the first of them while the weights are found (16 lanes a vector) ----
+  constexpr int T32 = WARPS * 32, IT = (PACK_VEC * D4 + T32 - 1) / T32;  // entries of a thread / 4
+  constexpr int MERGE = 20 / IT;
   float *wgt = (float *)smem;  // [nc][PACK_VEC]
   static_assert(PACK_MERGE * PACK_VEC * 4 <= WARPS * STAGES * 2 * HB, "within the rings");
   const size_t step = p.G;
   const float4 *src = (const float4 *)p.ws_o + slot0 * PACK_VEC * D4;
-  float4 y[MERGE];
-  auto fetch_sums = [&](int i, int k0) {
+  float4 y[IT][MERGE];
+  auto fetch_sums = [&](int k0) {
 #pragma unroll
-    for (int k = 0; k < MERGE; ++k)
-      if (k0 + k < nc) y[k] = __ldcg(src + i + (k0 + k) * step * PACK_VEC * D4);
-  };
-  if (i0 + tid < i1) fetch_sums(i0 + tid, 0);
-  if (i0 < i1)
-    for (int vi = i0 / D4 + warp; vi <= (i1 - 1) / D4; vi += WARPS) {
-      const float2 *part_ml = p.ws_ml + (slot0 * PACK_CLUSTER + rank) * PACK_VEC + vi;
-      float M = -INFINITY, L = 0.f;
-      for (int k = lane; k < nc; k += 32)
-        M = fmaxf(M, __ldcg(&part_ml[k * step * PACK_CLUSTER * PACK_VEC].x));
-#pragma unroll
-      for (int x = 16; x; x /= 2) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
-      for (int k = lane; k < nc; k += 32) {
-        const float2 ml = __ldcg(&part_ml[k * step * PACK_CLUSTER * PACK_VEC]);
-        const float f = merge_weight(ml.x, ml.y, M);
-        wgt[k * PACK_VEC + vi] = f;
-        L += f * ml.y;
-      }
-#pragma unroll
-      for (int x = 16; x; x /= 2) L += __shfl_xor_sync(0xFFFFFFFFu, L, x);
-      if (lane == 0) s_tot[vi] = make_float2(M, L);
-    }
-  __syncthreads();
-  for (int i = i0 + tid; i < i1; i += WARPS * 32) {
-    const int vi = i / D4;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = 0; k0 < nc; k0 += MERGE) {
-      if (k0 || i != i0 + tid) fetch_sums(i, k0);
+    for (int t = 0; t < IT; ++t)
 #pragma unroll
       for (int k = 0; k < MERGE; ++k)
-        if (k0 + k < nc) add4(x, wgt[(k0 + k) * PACK_VEC + vi], y[k]);
+        if (i0 + tid + t * T32 < i1 && k0 + k < nc)
+          y[t][k] = __ldcg(src + i0 + tid + t * T32 + (k0 + k) * step * PACK_VEC * D4);
+  };
+  fetch_sums(0);
+  if (tid < 16 * PACK_VEC) {
+    const int vi = tid >> 4, l16 = tid & 15;
+    const int n = i0 < i1 && vi >= i0 / D4 && vi <= (i1 - 1) / D4 ? nc : 0;
+    const float2 *part_ml = p.ws_ml + (slot0 * PACK_CLUSTER + rank) * PACK_VEC + vi;
+    auto part_of = [&](int k) {
+      return k < n ? __ldcg(&part_ml[k * step * PACK_CLUSTER * PACK_VEC])
+                   : make_float2(-INFINITY, 0.f);
+    };
+    const float2 first = part_of(l16), second = part_of(l16 + 16);
+    float M = fmaxf(first.x, second.x), L = 0.f;
+    for (int k = l16 + 32; k < n; k += 16) M = fmaxf(M, part_of(k).x);
+#pragma unroll
+    for (int x = 8; x; x /= 2) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, x));
+    for (int k = l16; k < n; k += 16) {
+      const float2 ml = k < 16 ? first : k < 32 ? second : part_of(k);
+      const float f = merge_weight(ml.x, ml.y, M);
+      wgt[k * PACK_VEC + vi] = f;
+      L += f * ml.y;
     }
-    out4(i, x, s_tot[vi].y);
+#pragma unroll
+    for (int x = 8; x; x /= 2) L += __shfl_xor_sync(0xFFFFFFFFu, L, x);
+    if (l16 == 0) s_tot[vi] = make_float2(M, L);
+  }
+  __syncthreads();
+  float4 x[IT];
+#pragma unroll
+  for (int t = 0; t < IT; ++t) x[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < nc; k0 += MERGE) {
+    if (k0) fetch_sums(k0);
+#pragma unroll
+    for (int t = 0; t < IT; ++t) {
+      const int i = i0 + tid + t * T32;
+#pragma unroll
+      for (int k = 0; k < MERGE; ++k)
+        if (i < i1 && k0 + k < nc) add4(x[t], wgt[(k0 + k) * PACK_VEC + i / D4], y[t][k]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < IT; ++t) {
+    const int i = i0 + tid + t * T32;
+    if (i < i1) out4(i, x[t], s_tot[i / D4].y);
   }
 }
 
