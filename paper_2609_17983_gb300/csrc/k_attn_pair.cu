@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(NT, 1)
       }
       if (dead) continue;
       // a row that has seen no key yet (another split's) keeps P = 0
-      const float nm = m == -INFINITY ? 0.f : -m;
+      const float nm = m == -INFINITY ? 0.f : HALF ? HALF_LIFT - m : -m;
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < HK / 32; ++k) {

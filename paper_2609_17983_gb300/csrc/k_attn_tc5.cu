@@ -462,12 +462,14 @@ __global__ void __launch_bounds__(NT5, 1)
         if (dead) continue;
       }
       float e[HK];
+      const float base = HALF ? m - HALF_LIFT : m;
       if (unmasked) {
 #pragma unroll
-        for (int j = 0; j < HK; ++j) e[j] = ex2(__uint_as_float(sr[j]) - m);
+        for (int j = 0; j < HK; ++j) e[j] = ex2(__uint_as_float(sr[j]) - base);
       } else {
 #pragma unroll
-        for (int j = 0; j < HK; ++j) e[j] = key0 + j <= pv ? ex2(__uint_as_float(sr[j]) - m) : 0.f;
+        for (int j = 0; j < HK; ++j)
+          e[j] = key0 + j <= pv ? ex2(__uint_as_float(sr[j]) - base) : 0.f;
       }
       {  // P in bf16 pairs: this part's HK keys are HK / 2 columns of buffer b
         uint32_t w[HK / 2];

@@ -48,7 +48,6 @@ using namespace ptx;
 
 constexpr int STAGES = 2;           // pages in flight per warp
 constexpr float RAISE = 8.f;        // headroom of the reference (log2)
-constexpr float LIFT = 7.f;         // P = 2^(x - reference + LIFT) <= 2^15: more of a half's range
 constexpr int SPARSE_MAX = 128;     // listed blocks of a part
 
 // One contiguous copy into shared memory, counted at bar.
@@ -422,8 +421,8 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     }
     uint32_t ph[4][2], pl[SPLIT ? 4 : 1][2];  // fragments of P^T: 16 keys, lane's vector lg
     {
-      const float base[2] = {LIFT - (ref[0] == -INFINITY ? 0.f : ref[0]),
-                             LIFT - (ref[1] == -INFINITY ? 0.f : ref[1])};
+      const float base[2] = {HALF_LIFT - (ref[0] == -INFINITY ? 0.f : ref[0]),
+                             HALF_LIFT - (ref[1] == -INFINITY ? 0.f : ref[1])};
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll

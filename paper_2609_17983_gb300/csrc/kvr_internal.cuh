@@ -658,7 +658,7 @@ const char *launch_attention_combine(const int4 *blocks, int n_blocks, int max_r
 // by a block's document (blocks[].w), tmaps 64-byte aligned.  tail_page: logical pages
 // from it on lie in another pool, with view and TMA view tail_docs entries further.
 // half_ldq > 0 (both kernels): the pages are halves, q's rows (bf16) half_ldq entries
-// apart; q goes as halves scaled by a power of two, and P is rounded to a half.
+// apart; q goes as halves scaled by a power of two, and P, lifted by 2^7, is rounded to a half.
 int attn_tc5_rows_per_block(int grp);
 int attn_tc5_ctas_per_sm(int dh);
 constexpr int NO_TAIL = 0x7fffffff;

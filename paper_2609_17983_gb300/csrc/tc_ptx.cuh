@@ -19,6 +19,11 @@ __device__ __forceinline__ float exp2_of(int e) {
 __device__ __forceinline__ int half_exponent(float a) {
   return min(max((int)(__float_as_uint(a) >> 23) - 127, -100), 126) - 8;
 }
+// Softmax weights that go as halves are 2^(x - reference + HALF_LIFT): with a headroom of the
+// reference of 8 at most 2^15, so that a half's 11 bits reach down to 2^-20 of the largest
+// weight or less (its least normal is 2^-14) and its last step is 2^-24 under that 2^6.
+constexpr float HALF_LIFT = 7.f;
+
 // The largest magnitude of eight bf16 (a NaN is passed over), and two as halves times f.
 __device__ __forceinline__ float bf16_magnitude(uint4 x) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
