@@ -16,8 +16,10 @@
 //                  vote instead of a reduction; the sums stay apart until the end;
 //   O^T += V^T P^T P in half, its fragments transposed by movmatrix; V^T like K.
 // q is scaled by a power of two per vector so that it is a half as exactly as it
-// was a bf16; an fp32 model's q and P go as two halves each (22 bits), with
-// a page's products added to O in fp32 registers.  All sums are in fp32.
+// was a bf16; an fp32 model's q and P go as two halves each (22 bits; P's second 2^11 above
+// the first, so that a small weight, whose first is subnormal or zero, keeps its bits down
+// to 2^-43 of the largest), with a page's products added to O in fp32 registers.  All sums
+// are in fp32.
 // The warps' (max, sum, O) meet in shared memory; those of a cluster's CTAs are brought
 // into the memory of the CTA that adds the slice (0.5 us sooner than read from there: a
 // token over 5000 positions 6.9 to 6.4); of several clusters the last to arrive adds
@@ -48,6 +50,7 @@ using namespace ptx;
 
 constexpr int STAGES = 2;           // pages in flight per warp
 constexpr float RAISE = 8.f;        // headroom of the reference (log2)
+constexpr float LOW = 2048.f;       // what the second half of a weight is lifted by
 constexpr int SPARSE_MAX = 128;     // listed blocks of a part
 
 // One contiguous copy into shared memory, counted at bar.
@@ -433,7 +436,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
           ph[kt][h] = transpose8x8(u);
           if (SPLIT) {
             const float2 f = __half22float2(*(const __half2 *)&u);
-            pl[kt][h] = transpose8x8(half2_of(x - f.x, y - f.y));
+            pl[kt][h] = transpose8x8(half2_of((x - f.x) * LOW, (y - f.y) * LOW));
             l[0] += x;
             l[1] += y;
           }
@@ -454,18 +457,18 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
       const uint4 x4 = vs16[b * 4 + lt], y4 = vs16[4 * DB + b * 4 + lt];
       const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
       const uint32_t vs[8] = {x4.x, x4.y, x4.z, x4.w, y4.x, y4.y, y4.z, y4.w};
-      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      float acc[4] = {0.f, 0.f, 0.f, 0.f}, low[4] = {0.f, 0.f, 0.f, 0.f};
       float *d = SPLIT ? acc : o[b];
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
         uint32_t a[4];
         v_fragment(w[kt], vs[2 * kt], vs[2 * kt + 1], a);
         mma16816(d, a, ph[kt][0], ph[kt][1]);
-        if (SPLIT) mma16816(d, a, pl[kt][0], pl[kt][1]);
+        if (SPLIT) mma16816(low, a, pl[kt][0], pl[kt][1]);
       }
       if (SPLIT) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[b][i] += acc[i];
+        for (int i = 0; i < 4; ++i) o[b][i] += fmaf(low[i], 1.f / LOW, acc[i]);
       }
     }
     // what was written here comes before the copies into the same memory

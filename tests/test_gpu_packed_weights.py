@@ -18,7 +18,8 @@ def allowed(dtype, ref, w, count, total, mean, gap):
 
     A weight is rounded to 11 bits, the smallest to steps of half's subnormals, 2^-24, where the
     largest weight is 2^6 at least: off by w 2^-11 or 2^-31.  fp32: in two halves, 22 bits or,
-    with the second 2^12 above the first, 2^-43.  It moves the numerator and may move the sum.
+    with the second 2^11 above the first and the largest weight 2^7 at least, 2^-43.  It moves
+    the numerator and may move the sum.
     A score is off by 16 roundings of itself, an exponential by 2^-19, of the numerator and of
     the sum.  The sums are of 32 bits: fewer than count / 8 + 64 additions on the way of a
     key.  The output is rounded to its type."""
@@ -31,6 +32,8 @@ def allowed(dtype, ref, w, count, total, mean, gap):
 
 @pytest.mark.parametrize("shape,dtype,n,R,many", [
     ("dh128", "bf16", 4096, 1, False), ("dh64", "bf16", 1500, 9, False),
+    ("dh128", "fp32", 4096, 1, False), ("dh64", "fp32", 1500, 9, False),
+    ("dh128", "fp32", 20000, 3, False),
     ("dh128", "bf16", 12345, 36, True), ("dh128", "bf16", 12345, 300, True),
     ("dh64", "bf16", 8000, 1201, True)])
 def test_a_dominating_key(models, shape, dtype, n, R, many):  # noqa: F811
