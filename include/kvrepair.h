@@ -325,7 +325,8 @@ void kvr_rows_free(kvr_rows *rows);
  * dtype, ldq elements apart (at least n_heads * head_dim, a whole number of 16-byte
  * pieces); out [rows][n_heads][head_dim], not overlapping q.  A row that sees a
  * key or value row stored as NaN is NaN for that head; one that does not see it
- * is untouched by it.  Errors: KVR_E_INVAL (a document freed since, pointers, ldq),
+ * is untouched by it.  A head whose q holds a NaN or an infinity is NaN where the row sees
+ * a key.  Errors: KVR_E_INVAL (a document freed since, pointers, ldq),
  * KVR_E_RANGE (layer), KVR_E_POISONED, KVR_E_NOMEM. */
 kvr_status kvr_packed_attention(kvr_rows *rows, int32_t layer, const void *q, int32_t ldq,
                                 void *out);

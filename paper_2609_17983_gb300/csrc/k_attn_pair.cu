@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(NT, 1)
         m = hand_over(m, [](float a, float b) { return fmaxf(a, b); });
         const int e = half_exponent(m);
 #pragma unroll
-        for (int k = 0; k < QP; ++k) x[k] = halves_of(x[k], exp2_of(-e));
+        for (int k = 0; k < QP; ++k) x[k] = halves_of(x[k], half_factor(m, e));
         qk_scale *= exp2_of(e);
       }
       const uint32_t q0 = sQ + t * QBYTES + v * 128;

@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(NT5, 1)
         quad_bar();
         const int e = half_exponent(mq_part);
 #pragma unroll
-        for (int k = 0; k < QW; ++k) w[k] = halves_of(w[k], exp2_of(-e));
+        for (int k = 0; k < QW; ++k) w[k] = halves_of(w[k], half_factor(mq_part, e));
         qk_scale *= exp2_of(e);
       }
 #pragma unroll

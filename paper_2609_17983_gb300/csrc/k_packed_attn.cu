@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm<T>(WARPS))
     a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
     a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
     const int e = half_exponent(a);
-    const float down = exp2_of(-e);
+    const float down = half_factor(a, e);
     qscale = exp2_of(e) * p.scale;
 #pragma unroll
     for (int b = 0; b < DB; ++b) {

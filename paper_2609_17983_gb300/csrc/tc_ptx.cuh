@@ -6,19 +6,26 @@
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_fp16.h>
+#include <math.h>
 
 namespace kvr {
 namespace ptx {
 
-// 2^e for e in [-126, 127], and the exponent e whose 2^-e brings magnitudes up to a (finite)
-// into [2^8, 2^9): bf16 entries are halves then as exactly as they were bf16, but for
-// those below 2^-32 of a.
+// 2^e for e in [-126, 127], and the exponent e whose 2^-e brings the largest magnitude a into
+// [2^8, 2^9): bf16 entries are halves then as exactly as they were bf16 down to 2^-25 of a
+// (a half's last step is 2^-24, a bf16 has eight bits); smaller ones are off by 2^-33 of it.
 __device__ __forceinline__ float exp2_of(int e) {
   return __uint_as_float((uint32_t)(127 + e) << 23);
 }
 __device__ __forceinline__ int half_exponent(float a) {
   return min(max((int)(__float_as_uint(a) >> 23) - 127, -100), 126) - 8;
 }
+// That 2^-e, or NaN where a is infinite: a query with an infinite entry has NaN scores alone (as
+// infinities of one sign they would not count, and the row would come out as zeros).
+__device__ __forceinline__ float half_factor(float a, int e) {
+  return a == INFINITY ? NAN : exp2_of(-e);
+}
+
 // Softmax weights that go as halves are 2^(x - reference + HALF_LIFT): with a headroom of the
 // reference of 8 at most 2^15, so that a half's 11 bits reach down to 2^-20 of the largest
 // weight or less (its least normal is 2^-14) and its last step is 2^-24 under that 2^6.
