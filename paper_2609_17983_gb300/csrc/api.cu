@@ -1950,7 +1950,7 @@ kvr_status kvr_packed_logits(kvr_model *m, kvr_packed *c, const int32_t *query, 
     if (!st) st = packed_pass(c, P, c->n + qm, n_blocks, false, launched);
     // the bounds of the document's last block were taken with the query's rows
     if (launched && c->n % KVR_PAGE) {
-      launch_packed_bounds(c->view(), c->n / KVR_PAGE, c->n, dm.L, m->stream);
+      launch_packed_bounds(c->view(), c->n / KVR_PAGE, c->n, dm.L, 0, 0, m->stream);
       const kvr_status s2 = launch_check(m, 1);
       if (!st) st = s2;
     }

@@ -440,16 +440,22 @@ __global__ void __launch_bounds__(2 * DH, sizeof(T) == 2 ? 512 / DH : 256 / DH)
   block_bounds<DH>(amax, kb, present, v.bounds + at * 2 * DH, v.unit + at);
 }
 
-// The bounds of a page alone.  Grid (G, layers), DH / 2 threads.
+// The bounds of a page alone, of the layers but [l0, l1).  Grid (G, layers), DH / 2 threads.
 template <int DH>
 __global__ void __launch_bounds__(DH / 2)
-    k_packed_bounds(const PackedView v, int page, int present) {
+    k_packed_bounds(const PackedView v, int page, int present, int l0, int l1) {
   __shared__ float amax[2];
   pdl_trigger();
   pdl_wait();
-  const size_t at = v.index(blockIdx.y, blockIdx.x, page);
-  block_bounds<DH>(amax, v.block(blockIdx.y, blockIdx.x, page), present, v.bounds + at * 2 * DH,
-                   v.unit + at);
+  const int g = blockIdx.x, l = (int)blockIdx.y < l0 ? blockIdx.y : blockIdx.y + l1 - l0;
+  const size_t at = v.index(l, g, page);
+  block_bounds<DH>(amax, v.block(l, g, page), present, v.bounds + at * 2 * DH, v.unit + at);
+}
+
+// The units of blocks of zeros.
+__global__ void k_packed_units(float *unit, size_t n) {
+  const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n) unit[i] = unit_of(0.f);
 }
 
 // Pages that a call writes in part: a CTA per (KV head, page, layer).  The new rows are
@@ -1082,10 +1088,15 @@ void launch_packed_read(const PackedView &v, int dtype, const PackedRows &rows, 
   });
 }
 
-void launch_packed_bounds(const PackedView &v, int page, int len, int nl, cudaStream_t s) {
+void launch_packed_bounds(const PackedView &v, int page, int len, int nl, int l0, int l1,
+                          cudaStream_t s) {
   const int present = std::min(KVR_PAGE, len - page * KVR_PAGE);
-  launch_pdl(v.dh == 128 ? k_packed_bounds<128> : k_packed_bounds<64>, dim3(v.G, nl),
-             dim3(v.dh / 2), 0, s, v, page, present);
+  launch_pdl(v.dh == 128 ? k_packed_bounds<128> : k_packed_bounds<64>, dim3(v.G, nl - (l1 - l0)),
+             dim3(v.dh / 2), 0, s, v, page, present, l0, l1);
+}
+
+void launch_packed_units(float *unit, size_t n, cudaStream_t s) {
+  k_packed_units<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(unit, n);
 }
 
 void launch_packed_unpack(const PackedView &v, int layer, int n_pages, void *pages, bool settled,

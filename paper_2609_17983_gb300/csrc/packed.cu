@@ -482,10 +482,14 @@ kvr_status kvr_packed_create(kvr_model *m, int32_t capacity, kvr_packed **out) {
       return fail(KVR_E_NOMEM, "packed cache of %d positions", capacity);
     }
     if (cudaMemsetAsync(c->blocks, 0, block_b, m->stream) != cudaSuccess ||
-        cudaMemsetAsync(c->bounds, 0, bound_b, m->stream) != cudaSuccess ||
-        cudaMemsetAsync(c->unit, 0, n * sizeof(float), m->stream) != cudaSuccess) {
+        cudaMemsetAsync(c->bounds, 0, bound_b, m->stream) != cudaSuccess) {
       kvr_packed_free(c);
       return fail(KVR_E_CUDA, "packed cache clear");
+    }
+    launch_packed_units(c->unit, n, m->stream);
+    if (const kvr_status st = launched(m, 1, "packed cache clear")) {
+      kvr_packed_free(c);
+      return st;
     }
     *out = c;
     return KVR_OK;
@@ -529,9 +533,14 @@ kvr_status kvr_packed_write(kvr_packed *c, const int32_t *positions, int32_t n_p
     PackedRows rows;
     KVR_TRY(rows_of(m, positions, n_pos, rows));
     const int len = std::max(c->n, positions[n_pos - 1] + 1);
-    const int n =
-        launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->num_sms,
-                            m->stream);
+    int n = launch_packed_write(c->view(), m->dims.dtype, rows, len, l0, l1 - l0, k, v, m->num_sms,
+                                m->stream);
+    // the other layers hold zeros at the new positions: no write of theirs takes the bounds of
+    // the block that the length ended in (those behind it are blocks of zeros)
+    if (len > c->n && c->n % KVR_PAGE && l1 - l0 < m->dims.L) {
+      launch_packed_bounds(c->view(), c->n / KVR_PAGE, len, m->dims.L, l0, l1, m->stream);
+      ++n;
+    }
     const kvr_status st = launched(m, n, "packed write");
     if (st)
       c->poisoned = true;

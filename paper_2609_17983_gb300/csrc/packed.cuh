@@ -312,7 +312,11 @@ kvr_status packed_rows_of(kvr_model *m, const int32_t *pos, int n, PackedRows &r
 kvr_status packed_pass_rows(kvr_packed *c, const int32_t *pos, int n, kvr_rows **out);
 // Attention of layer `layer` over all positions, or (n_blocks > 0) the selected blocks.
 kvr_status packed_attend(kvr_rows *r, int layer, const void *q, void *out, int n_blocks);
-// The bounds of one page of layers [0, nl) over its slots below the length len.
-void launch_packed_bounds(const PackedView &v, int page, int len, int nl, cudaStream_t s);
+// The bounds of one page over its slots below the length len, of layers [0, nl) without
+// [l0, l1).
+void launch_packed_bounds(const PackedView &v, int page, int len, int nl, int l0, int l1,
+                          cudaStream_t s);
+// The units of n blocks of zeros.
+void launch_packed_units(float *unit, size_t n, cudaStream_t s);
 
 }  // namespace kvr
