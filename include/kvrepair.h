@@ -368,8 +368,9 @@ kvr_status kvr_packed_repair(kvr_packed *packed, const int32_t *new_tokens, int3
 
 /* kvr_logits on a packed document: the query's m tokens attend, at positions n.., to all
  * positions (n_blocks == 0) or, in every layer, to the n_blocks blocks that
- * kvr_packed_select picks for each row.  Their own K/V are quantised behind the document,
- * whose entries, bounds and length stay as they were.  Synchronous.  Errors as
+ * kvr_packed_select picks for each row.  Their own K/V are quantised behind the document
+ * and cleared again: its entries, bounds and length, and the zeros behind it, are then as
+ * they were.  Synchronous.  Errors as
  * kvr_logits and kvr_packed_repair; KVR_E_RANGE for n_blocks outside [0, 16384]. */
 kvr_status kvr_packed_logits(kvr_model *model, kvr_packed *packed, const int32_t *query, int32_t m,
                              int32_t n_blocks, float *logits_out);

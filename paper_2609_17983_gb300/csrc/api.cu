@@ -1948,9 +1948,9 @@ kvr_status kvr_packed_logits(kvr_model *m, kvr_packed *c, const int32_t *query, 
     bool launched = false;
     kvr_status st = stage_add(m, c->tokens_d + c->n, query, qm);
     if (!st) st = packed_pass(c, P, c->n + qm, n_blocks, false, launched);
-    // the bounds of the document's last block were taken with the query's rows
-    if (launched && c->n % KVR_PAGE) {
-      launch_packed_bounds(c->view(), c->n / KVR_PAGE, c->n, dm.L, 0, 0, m->stream);
+    // nothing of the query's rows stays, in the positions behind or in the bounds
+    if (launched) {
+      launch_packed_clear(c->view(), c->n, c->n + qm, dm.L, m->stream);
       const kvr_status s2 = launch_check(m, 1);
       if (!st) st = s2;
     }

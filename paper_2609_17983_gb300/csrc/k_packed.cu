@@ -452,6 +452,42 @@ __global__ void __launch_bounds__(DH / 2)
   block_bounds<DH>(amax, v.block(l, g, page), present, v.bounds + at * 2 * DH, v.unit + at);
 }
 
+// The slots of positions from `len` on, in the pages from its own, as if nothing had been
+// written there: zeros, and the bounds over the slots before.  Grid (G, pages, layers),
+// 2 DH threads.
+template <int DH>
+__global__ void __launch_bounds__(2 * DH) k_packed_clear(const PackedView v, int len) {
+  constexpr int NT = 2 * DH, DB = DH / 16, DQ = DH / 64, CB = pack_code_bytes(DH),
+                HB = pack_half_bytes(DH);
+  __shared__ float amax[2];
+  pdl_trigger();
+  pdl_wait();
+  const int g = blockIdx.x, l = blockIdx.z, page = len / KVR_PAGE + blockIdx.y;
+  const int present = max(0, len - page * KVR_PAGE);
+  uint8_t *kb = v.block(l, g, page), *vb = kb + HB;
+  for (int i = threadIdx.x; i < CB / 4; i += NT) {
+    // K: [kt][db / 4][lane][db % 4], a key in each half of a word
+    const int key = 16 * (i / (128 * DQ)) + pack_key_of((i / 4 & 31) >> 2);
+    uint32_t *w = (uint32_t *)kb + i;
+    if (key >= present)
+      *w = 0;
+    else if (key + 2 >= present)
+      *w &= 0xFFFFu;
+    // V: [db][lane ^ db][kt], four keys in each half
+    const int key4 = 16 * (i & 3) + 4 * (((i / 4 & 31) ^ i / 128) & 3);
+    const int keep = min(4, max(0, present - key4));
+    ((uint32_t *)vb)[i] &= ((1u << (4 * keep)) - 1) * 0x00010001u;
+  }
+  for (int i = threadIdx.x; i < KVR_PAGE * DB; i += NT) {
+    const int key = i / DB, db = i % DB;
+    if (key >= present) kb[pack_k_scale(DH, key, db)] = vb[pack_v_scale(DH, key, db)] = 0;
+  }
+  __syncthreads();
+  if (threadIdx.x >= DH / 2) return;
+  const size_t at = v.index(l, g, page);
+  block_bounds<DH>(amax, kb, present, v.bounds + at * 2 * DH, v.unit + at);
+}
+
 // The units of blocks of zeros.
 __global__ void k_packed_units(float *unit, size_t n) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
@@ -1093,6 +1129,11 @@ void launch_packed_bounds(const PackedView &v, int page, int len, int nl, int l0
   const int present = std::min(KVR_PAGE, len - page * KVR_PAGE);
   launch_pdl(v.dh == 128 ? k_packed_bounds<128> : k_packed_bounds<64>, dim3(v.G, nl - (l1 - l0)),
              dim3(v.dh / 2), 0, s, v, page, present, l0, l1);
+}
+
+void launch_packed_clear(const PackedView &v, int len, int end, int nl, cudaStream_t s) {
+  launch_pdl(v.dh == 128 ? k_packed_clear<128> : k_packed_clear<64>,
+             dim3(v.G, (end - 1) / KVR_PAGE - len / KVR_PAGE + 1, nl), dim3(2 * v.dh), 0, s, v, len);
 }
 
 void launch_packed_units(float *unit, size_t n, cudaStream_t s) {

@@ -316,6 +316,9 @@ kvr_status packed_attend(kvr_rows *r, int layer, const void *q, void *out, int n
 // [l0, l1).
 void launch_packed_bounds(const PackedView &v, int page, int len, int nl, int l0, int l1,
                           cudaStream_t s);
+// Positions [len, end), the last ones with anything written, as if nothing had been: zeros,
+// and their blocks' bounds over the positions before; of layers [0, nl).
+void launch_packed_clear(const PackedView &v, int len, int end, int nl, cudaStream_t s);
 // The units of n blocks of zeros.
 void launch_packed_units(float *unit, size_t n, cudaStream_t s);
 

@@ -4,8 +4,9 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2609_17983_gb300 import synth
 from tests import packed_plain as pp
-from tests.test_gpu_packed import (SHAPES, check, f64, models, queries,  # noqa: F401
+from tests.test_gpu_packed import (SHAPES, TORCH, check, f64, kv, models, queries,  # noqa: F401
                                    read, rows, same)
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +55,35 @@ def test_layers_of_unequal_length(models, shape, dtype, steps):  # noqa: F811
         for l in range(2):
             check_layer(doc, m, l, k[l, :doc.n], v[l, :doc.n], dtype, H)
     doc.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,ask,blocks,grow", [(100, 8, 0, 1), (100, 8, 2, 28), (120, 40, 0, 30),
+                                               (128, 64, 3, 64), (127, 2, 0, 2)])
+def test_nothing_is_left_of_a_question(dtype, n, ask, blocks, grow):
+    """The rows of a question leave the positions behind the document as they were: zeros where a
+    write of one layer then lengthens it."""
+    if kv is None:
+        pytest.fail("no library")
+    cfg = synth.preset("tiny", dtype=dtype)
+    G, dh, L = cfg["n_kv_heads"], cfg["head_dim"], cfg["n_layers"]
+    m = kv.Model(cfg, None, seed=0, max_context=512, max_rows=64)
+    m.set_stream(torch.cuda.current_stream().cuda_stream)
+    cache = m.prefill(synth.document(1, n, cfg["vocab"]))
+    doc = m.pack(cache)
+    cache.close()
+    before = read(doc, np.arange(n), L, G, dh, dtype)
+    bounds = [doc.bounds(l) for l in range(L)]
+    first = m.packed_logits(doc, synth.fill_tokens(5, ask, cfg["vocab"], cfg["delim_id"]), blocks)
+    assert np.isfinite(first).all() and doc.n == n
+    for l in range(L):
+        assert all(same(a, b) for a, b in zip(doc.bounds(l), bounds[l]))
+    new = rows(3, grow, 1, G, dh, dtype)
+    doc.write(np.arange(n, n + grow), new, new, layer_begin=1, layer_end=2)
+    x = pp.stored(f64(new))[:, 0]
+    for l in range(L):
+        tail = x if l == 1 else np.zeros_like(x)
+        check_layer(doc, m, l, np.r_[before[0][:, l], tail], np.r_[before[1][:, l], tail], dtype,
+                    cfg["n_heads"])
+    doc.close()
+    m.close()
