@@ -997,7 +997,6 @@ kvr_status many_attention(kvr_model *m, const ManyPlan &p, const int4 *tables, c
   CUtensorMap tm;
   if (!make_tmap_bf16(&tm, pages, p.pages * 2 * dm.G * KVR_PAGE, dm.dh, KVR_PAGE))
     return fail(KVR_E_CUDA, "tensor map of unpacked pages");
-  Prof pr(m, P_ATTN, (int64_t)p.pages * KVR_PAGE * dm.G * dm.dh * 2 * 2);
   const char *e =
       p.n_pairs ? launch_attention_pair(q, pos, tables, p.n_blocks, tables + p.n_blocks, p.n_pairs,
                                         p.splits, dm, 0, identity, tm, m->attn_ws_o, m->attn_ws_ml,
