@@ -175,11 +175,14 @@ Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int
 // Whether the rows of a document at `pos` (ascending, >= 0) go by way of unpacked pages: one
 // kernel widens the layer's blocks to pages of halves, and the tcgen05 attention takes a tile of
 // 128 vectors at a time where the fused kernel takes 8.  Units are (page, tile of 8 vectors,
-// KV head); where the other way is shorter was fitted to 270 launches by both, of 8 to 4096 rows
-// over 512 to 12345 positions: the one taken is 0.2% slower than the other on average,
-// 17% at most.  40 rows spread over 5000 positions (28 heads) 17.3 us against 20.4, the
-// last 64 27.7 against 23.0; a chunk of 4096 rows over 12345 positions 2794 against 474.  A
-// second document is unpacked anew.
+// KV head); where the other way is shorter was fitted to launches by both, of 8 to 4096 rows
+// over 512 to 12345 positions.  One document (270 launches): the way taken is 0.3% slower than
+// the other on average, 24% at most (40 rows spread over 12345 positions, 32 heads: 38.1 us
+// by pages, 30.7 fused; over 5000, 28 heads, 20.6 and 15.5; the last 64 23.6 and 28.2; a
+// chunk of 4096 rows over 12345 480 and 2813).  Several, with as many rows each, share the
+// fused kernel's launch and are unpacked one after another (756 launches of 2, 4 and 8):
+// 0.4% and 32% (eight times the last 96 rows over 2000 positions, 28 heads: 159 us by pages,
+// 120 fused; two times 512 over 512, 32 heads, 31.0 and 54.2).
 bool many_rows(const kvr_model *m, const int32_t *pos, int rows, size_t docs) {
   const Dims &dm = m->dims;
   if (dm.dtype != KVR_DTYPE_BF16 || rows < 1) return false;
@@ -188,8 +191,11 @@ bool many_rows(const kvr_model *m, const int32_t *pos, int rows, size_t docs) {
   for (int v = 0; v < rows * grp; v += PACK_VEC)
     units += pos[std::min(rows * grp - 1, v + PACK_VEC - 1) / grp] / KVR_PAGE + 1;
   const long long n = pos[rows - 1] + 1;
-  const long long least = dm.dh == 128 ? 6600 + n * 2 / 5 : 5000 + n * 26 / 25;
-  return units * dm.G > least + (docs > 1 ? 5000 : 0);
+  const long long least = docs == 1 ? (dm.dh == 128 ? 6600 + n * 2 / 5 : 5000 + n * 26 / 25)
+                          : dm.dh == 128
+                              ? 7500 + n * 11 / 10
+                              : 7000 + n + 2000 * (long long)std::min<size_t>(docs, 8);
+  return units * dm.G > least;
 }
 
 // The tables of rows at `pos`, built and sent.
@@ -393,7 +399,10 @@ kvr_status select_blocks(kvr_rows *r, PackedAttnArgs &a, int n_blocks, int32_t *
   return KVR_OK;
 }
 
-// Attention over listed blocks.
+// Attention over listed blocks.  The deal is that of as many pages: over 350 launches of 1 to 64
+// rows with lists of 1 to 64 blocks (both types, both head sizes) it is 3.2% slower than the
+// fastest on average, 27% at most (40 rows of 64 blocks, fp32, 4 heads of 64: 15.6 us
+// against 11.9); 40 rows of 24 blocks, 28 heads 12.6 (the fastest 12.6).
 kvr_status attend_blocks(kvr_rows *r, PackedAttnArgs &a, const int32_t *blocks, int n_blocks,
                          void *out) {
   kvr_model *m = r->model;
