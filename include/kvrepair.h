@@ -290,7 +290,7 @@ int32_t kvr_packed_len(const kvr_packed *packed);
  * [layer_begin, layer_end) into the cache: k, v [n_pos][layers][n_kv_heads][head_dim].
  * Rewritten positions are replaced, and the bounds of the touched blocks are taken
  * anew over all their rows.  A layer whose rows of a position were not
- * written holds zeros there.  n_pos == 0 or no layers: nothing is done.  Errors: KVR_E_INVAL (NULL
+ * written holds zeros there, of which its bounds know.  n_pos == 0 or no layers: nothing is done.  Errors: KVR_E_INVAL (NULL
  * or not device memory, alignment), KVR_E_RANGE (layers, positions),
  * KVR_E_POISONED, KVR_E_NOMEM, KVR_E_CUDA (poisons the cache). */
 kvr_status kvr_packed_write(kvr_packed *packed, const int32_t *positions, int32_t n_pos,
@@ -326,8 +326,10 @@ void kvr_rows_free(kvr_rows *rows);
  * pieces); out [rows][n_heads][head_dim], not overlapping q.  A row that sees a
  * key or value row stored as NaN is NaN for that head; one that does not see it
  * is untouched by it.  A head whose q holds a NaN or an infinity is NaN where the row sees
- * a key.  Errors: KVR_E_INVAL (a document freed since, pointers, ldq),
- * KVR_E_RANGE (layer), KVR_E_POISONED, KVR_E_NOMEM. */
+ * a key.  Sums are in 32 bits; a bf16 model's weights are rounded to 11 bits (those
+ * below 2^-20 of the largest to steps of 2^-30 of it at most), an fp32 model's q and
+ * weights to 22 (below 2^-21 to steps of 2^-42).  Errors: KVR_E_INVAL (a document freed
+ * since, pointers, ldq), KVR_E_RANGE (layer), KVR_E_POISONED, KVR_E_NOMEM. */
 kvr_status kvr_packed_attention(kvr_rows *rows, int32_t layer, const void *q, int32_t ldq,
                                 void *out);
 

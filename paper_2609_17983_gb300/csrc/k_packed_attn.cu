@@ -29,8 +29,8 @@
 // 22.3 us at the copy rate, and takes 30.5; sixteen documents of 8191 positions the same
 // in 30.5.  Of that about 5 us are the launch, the first copy's way and the sums; between
 // them an SM's 12 warps take 12 pages in 2.5 us, 6.7 TB/s over the chip, while its
-// schedulers issue half the time (1000 instructions a page and warp, 450 of them
-// conversions and byte permutations in the ALU's half-rate pipe).  mma.sync serves because
+// schedulers issue half the time (918 instructions a page and warp, 256 of them
+// conversions of codes and 256 products with scales).  mma.sync serves because
 // eight columns are all there is: with 128 rows of a tcgen05 tile a token's heads
 // would leave 120 empty, and the widened keys would have to pass through shared memory.
 // Many rows go that way (many_attention).

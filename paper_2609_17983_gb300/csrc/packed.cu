@@ -136,12 +136,13 @@ struct Deal {
 // The deal whose launch is modelled to end first, in units of 10 ns.  A wave of CTAs costs
 // 2.8 us beside its rounds (a page for each of a CTA's warps), a round 1.5; a cluster's
 // sums 1.4, a merge through memory 2.5 and 0.07 per cluster; clusters of 8 leave 7/20 of
-// the SMs without a place.  Over 8500 launches of 1 to 64 rows over 64 to 131072 positions
-// the deal taken is 0.7% slower than the fastest on average, 13% at most.  One token over
-// 5000 positions, 4 KV heads: 8 CTAs of 12 warps as a cluster 6.4 us (merged through memory
-// 8.0, with 4 warps 7.6); over 131072, 8 KV heads: 19 CTAs of 12 warps a head 30.7 (in
-// clusters of 2 32.2); 16 documents of 8191: a CTA a document and head 31.1 (with 4 warps
-// 33.2).
+// the SMs without a place.  Of 8179 launches of 220 calls (1 to 64 rows over 64 to 131072
+// positions, up to 16 documents, both types) the deal taken is 3.4% slower than the fastest
+// of its call on average, 18% at most (three rows over 1125 positions, 4 heads: 5.2 us, in
+// clusters of 8 CTAs of 4 warps 4.4).  One token over 5000 positions, 4 KV heads: 8 CTAs
+// of 12 warps as a cluster 6.3 us (merged through memory 8.0, with 4 warps 7.6); over
+// 131072, 8 KV heads: 19 CTAs of 12 warps a head 30.7 (in clusters of 2 32.2); 16 documents
+// of 8191: a CTA a document and head 30.5 (with 4 warps 33.2).
 Deal deal(const kvr_model *m, const std::vector<std::pair<int, int>> &pages, int G) {
   const int many = m->dims.dtype == KVR_DTYPE_BF16 ? 12 : 8;
   int most = 1;
