@@ -251,7 +251,7 @@ def prepare(case, seed):
     st["out"] = torch.empty_like(st["q"])
     if case["op"] == "weigh":
         st["weight"] = torch.empty((D, 1, G, n), dtype=torch.float32, device="cuda")
-        st["each"] = list(st["weight"])
+        st["number"] = torch.empty((D, 1, G, n), dtype=torch.int32, device="cuda")
     return st
 
 
@@ -352,8 +352,8 @@ def run(st):
             st["rows"].attention(0, st["q"], st["out"])
             return {"out": st["out"]}
         st["rows"].attention(0, st["q"], st["out"], weigh=0.0)
-        for doc, weight in zip(st["docs"], st["each"]):
-            doc.entries(weight_out=weight)
+        for doc, number, weight in zip(st["docs"], st["number"], st["weight"]):
+            doc.entries(number, weight)
         return {"out": st["out"], "weight": st["weight"]}
     dt = _torch_dtype(case)
     if op == "store":
