@@ -116,6 +116,13 @@ __device__ __forceinline__ uint4 recode(uint4 c, float f) {
   return make_uint4(word(c.x), word(c.y), word(c.z), word(c.w));
 }
 
+// The factor of kept codes from their block's power to the new one.  A code that is not zero, 2^-9 or
+// more, makes the new power at least 2^-17 of the old one; zeros alone may meet a quotient of up to
+// 2^220, which is infinite and would make them NaN.
+__device__ __forceinline__ float kept_factor(float old, float power) {
+  return fminf(old * c8_inverse(power), 131072.f);
+}
+
 // Where a thread of a block's CTA of N works: piece `c` of the rows `row + j * STEP`.
 template <int DH, int N>
 struct Place {
@@ -438,9 +445,9 @@ __global__ void __launch_bounds__(KEEP_NT)
       for (int j = 0; j < P::ROWS; ++j) {
         const int slot = at.slot(j), o = at.offset(slot);
         if (e0 + slot >= n) continue;
-        *(uint4 *)(to + o) = power[j].x == pk ? x[j] : recode(x[j], power[j].x * c8_inverse(pk));
+        *(uint4 *)(to + o) = power[j].x == pk ? x[j] : recode(x[j], kept_factor(power[j].x, pk));
         *(uint4 *)(to + o + c8_half_bytes(DH)) =
-            power[j].y == pv ? y[j] : recode(y[j], power[j].y * c8_inverse(pv));
+            power[j].y == pv ? y[j] : recode(y[j], kept_factor(power[j].y, pv));
       }
       if (tid < KVR_PAGE && e0 + tid < n) {
         dst.number[d0 * KVR_PAGE + e0 + tid] = number;

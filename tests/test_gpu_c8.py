@@ -620,6 +620,43 @@ def test_keep(models, shape, dtype, n, keep):
     other.c.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", ["dh64", "dh128"])
+@pytest.mark.parametrize("e", [27, 28, 40, 119])
+def test_keep_zeros_of_large_powers(models, shape, dtype, e):
+    """Two blocks whose entries were rounded to zero under one magnitude each, K's in one layer and
+    V's in the other; that magnitude dropped, so that zeros move to the least power or beside tiny
+    entries.  They stay zeros, into another cache and in place, and attention is finite."""
+    m, n = models(shape, dtype), 200
+    p = Pair(m, shape, dtype, n)
+    k, v = (rows(s, n, 2, p.G, p.dh, dtype) for s in (41, 42))
+    for x, l in ((k, 0), (v, 1)):
+        x[[5, 70], l, :, 3] = 448 * 2.0 ** e  # the block's power is 2^e
+        x[128:, l] *= 2.0 ** -60
+    p.write(np.arange(n), k, v)
+    p.check()
+    at = np.setdiff1d(np.arange(n), [5, 70])
+    kept = torch.as_tensor(at, dtype=torch.int32).repeat(2, p.G, 1).cuda()
+    other = m.cache8(len(at))
+    p.c.keep(kept, into=other)
+    p.keep(kept.cpu().numpy())
+    assert not p.plain[0][0].k[:120].any() and not p.plain[1][0].v[:120].any()
+    p.check(other)
+    p.c.keep(kept)
+    p.check()
+    seen = np.array([3, 63, 100, len(at) - 1])
+    r = m.rows8([(p.c, seen)])
+    q = queries(43, len(seen), p.H, p.dh, dtype)
+    out = torch.empty_like(q)
+    for l in range(2):
+        r.attention(l, q, out, weigh=0.0)
+        assert torch.isfinite(out).all()
+        check_attention(p, l, q, seen, out, weights_of(p.c, l, len(at), p.G))
+    r.close()
+    other.close()
+    p.c.close()
+
+
 def test_keep_lists_of_the_caller(models):
     """Entries outside the cache or out of order are kept as zeros that have no number."""
     m = models("dh64", "bf16")
