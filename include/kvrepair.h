@@ -462,7 +462,7 @@ void kvr_c8_rows_free(kvr_c8_rows *rows);
  * weights are rounded to 11 bits (those below 2^-20 of the largest to steps of 2^-30 of it at
  * most), an fp32 model's q and weights to 22 (below 2^-21 to steps of 2^-42).  In calls of many rows of
  * a bf16 model, keys and values of blocks whose power is below 2^-22 of the largest one of the KV head
- * (up to the last row's entry) are rounded to 2^-32 of that.  Errors: KVR_E_INVAL (a document
+ * (up to the last row's entry) are off by up to 2^-32 of that.  Errors: KVR_E_INVAL (a document
  * freed since, pointers, ldq), KVR_E_RANGE (layer, a row's entry that its layer does not
  * hold), KVR_E_POISONED, KVR_E_NOMEM. */
 kvr_status kvr_c8_attention(kvr_c8_rows *rows, int32_t layer, const void *q, int32_t ldq, void *out);

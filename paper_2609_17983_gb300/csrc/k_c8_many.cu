@@ -19,6 +19,27 @@ using namespace ptx;
 // value is off by at most 2^-32 of it.
 constexpr float LIFT = 128.f, LIFT_INV = 1.f / 128.f;
 
+// That factor of a page's codes as halves.  From 2^-24 on (powers 2^-31 of the largest) it is one, and a
+// product rounds once.  Below it is `low`: codes are first taken 2^-15 down, which is exact, then
+// multiplied by the factor 2^15 up, which rounds once, too (where that is none either, below 2^-39,
+// all products round to zero).
+struct HalfFactor {
+  __half2 down, f;
+  bool low;
+  __device__ __forceinline__ explicit HalfFactor(float x) : low(x < 5.9604644775390625e-8f) {
+    down = __float2half2_rn(low ? 1.f / 32768.f : 1.f);
+    f = __float2half2_rn(low ? x * 32768.f : x);
+  }
+};
+// LOW: some factor of a warp's codes may be low.
+template <bool LOW>
+__device__ __forceinline__ uint32_t times(uint32_t codes, const HalfFactor &h) {
+  __half2 x = *(const __half2 *)&codes;
+  if (LOW) x = __hmul2(x, h.down);
+  x = __hmul2(x, h.f);
+  return *(const uint32_t *)&x;
+}
+
 // The largest powers of the first n pages of a head, by all NT threads of a CTA; s: shared, 0 before.
 template <int N>
 __device__ __forceinline__ float2 largest_powers(const float2 *powers, int n, uint32_t *s) {
@@ -103,17 +124,15 @@ struct Widen {
   __device__ __forceinline__ uint4 load(const uint8_t *a, const uint8_t *b, int j) const {
     return *(const uint4 *)((j < EACH / 2 ? a : b) + from + j % (EACH / 2) * (STEP * DH));
   }
-  // under the power of two f
-  __device__ __forceinline__ void store(uint32_t tile, uint4 u, __half2 f, int j) const {
+  template <bool LOW>
+  __device__ __forceinline__ void store(uint32_t tile, uint4 u, const HalfFactor &f, int j) const {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
     uint32_t o[8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       c8_halves(w[k], o[2 * k], o[2 * k + 1]);
-      const __half2 x = __hmul2(*(const __half2 *)&o[2 * k], f),
-                    y = __hmul2(*(const __half2 *)&o[2 * k + 1], f);
-      o[2 * k] = *(const uint32_t *)&x;
-      o[2 * k + 1] = *(const uint32_t *)&y;
+      o[2 * k] = times<LOW>(o[2 * k], f);
+      o[2 * k + 1] = times<LOW>(o[2 * k + 1], f);
     }
     *(uint4 *)__cvta_shared_to_generic(tile + to0 + j * (STEP * 128)) =
         make_uint4(o[0], o[1], o[2], o[3]);
@@ -408,11 +427,19 @@ __global__ void __launch_bounds__(NTR, 1) k_c8_rows(const __grid_constant__ C8Ro
                         (i < 2 || mbar_wait(&empty[b], ph ^ 1, abort_v, p.dev_flag, 84));
         if (!__all_sync(0xffffffffu, ok)) break;
         const uint8_t *codes = raw + st * BB;
-        const __half2 ha = __float2half2_rn(fa), hb = __float2half2_rn(fb);
+        const HalfFactor ha(fa), hb(fb);
+        auto widen = [&](auto low) {
 #pragma unroll
-        for (int j = 0; j < Widen<DH, N>::EACH; ++j)
-          w.store(tile + b * TBYTES, w.load(codes, codes + BB / 2, j),
-                  j < Widen<DH, N>::EACH / 2 ? ha : hb, j);
+          for (int j = 0; j < Widen<DH, N>::EACH; ++j)
+            w.template store<low>(tile + b * TBYTES, w.load(codes, codes + BB / 2, j),
+                                  j < Widen<DH, N>::EACH / 2 ? ha : hb, j);
+        };
+        // (both products for all pages: 64 rows over 16384 27.4 us, 512 over 5000 48.7; as it is 26.7
+        // and 47.4)
+        if (ha.low || hb.low)
+          widen(std::true_type{});
+        else
+          widen(std::false_type{});
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
@@ -898,21 +925,25 @@ __global__ void __launch_bounds__(NT, 1)
       // (the products of the pair before are done: this warp has seen the last one's scores)
       const int t0 = s_first[k];
       if (t0 < t1) {
-        const __half2 f = __float2half2_rn(power * down);
+        const HalfFactor f(power * down);  // (a warp's keys are of one page)
+        auto store = [&](auto low) {
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-          const uint32_t w[4] = {codes[j].x, codes[j].y, codes[j].z, codes[j].w};
-          uint32_t o[8];
+          for (int j = 0; j < EACH; ++j) {
+            const uint32_t w[4] = {codes[j].x, codes[j].y, codes[j].z, codes[j].w};
+            uint32_t o[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            c8_halves(w[i], o[2 * i], o[2 * i + 1]);
-            const __half2 x = __hmul2(*(const __half2 *)&o[2 * i], f),
-                          y = __hmul2(*(const __half2 *)&o[2 * i + 1], f);
-            o[2 * i] = *(const uint32_t *)&x;
-            o[2 * i + 1] = *(const uint32_t *)&y;
+            for (int i = 0; i < 4; ++i) {
+              c8_halves(w[i], o[2 * i], o[2 * i + 1]);
+              o[2 * i] = times<low>(o[2 * i], f);
+              o[2 * i + 1] = times<low>(o[2 * i + 1], f);
+            }
+            tmem_st8_nowait(tl + S_SLOTS * TILE + u * (DH / 2) + (half * EACH + j) * 8, o);
           }
-          tmem_st8_nowait(tl + S_SLOTS * TILE + u * (DH / 2) + (half * EACH + j) * 8, o);
-        }
+        };
+        if (f.low)
+          store(std::true_type{});
+        else
+          store(std::false_type{});
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         __syncwarp();
