@@ -328,6 +328,26 @@ kvr_status attn_workspace(kvr_model *m, const kvr_c8_rows::Plan &p, C8AttnArgs &
   return KVR_OK;
 }
 
+// What the many rows of a document lay out in the pages' scratch: two sets of powers, the pages of halves,
+// the vectors and what makes weights of their products, the runs' sums (those for weights alone).
+struct ManyScratch {
+  size_t powers, vectors, factors, last, partial, all;  // offsets from the second set of powers on
+};
+ManyScratch many_scratch(const Dims &dm, const kvr_c8_rows::Many &x, bool weigh) {
+  const size_t pages_b = x.straight ? 0 : up256((size_t)x.plan.pages * 2 * dm.G * KVR_PAGE * dm.dh * 2),
+               vec = (size_t)dm.G * x.shape.nv_pad;
+  ManyScratch y;
+  y.powers = up256(dm.G * sizeof(float2));
+  y.vectors = 2 * y.powers + pages_b;
+  y.factors = y.vectors + vec * dm.dh * 2;
+  y.last = y.factors + vec * 12;
+  y.partial = y.last + vec * 4;
+  const size_t partial_b =
+      x.shape.runs > 1 ? (size_t)x.shape.runs * dm.G * x.shape.keys * 4 : 0;
+  y.all = weigh ? y.partial + partial_b : y.vectors;
+  return y;
+}
+
 // The many rows of one document.  stats: [rows][H] of all rows, or null: without weights.
 kvr_status attend_many(kvr_c8_rows *r, const kvr_c8_rows::Many &x, const C8AttnArgs &a, float2 *stats,
                        float decay) {
@@ -335,15 +355,9 @@ kvr_status attend_many(kvr_c8_rows *r, const kvr_c8_rows::Many &x, const C8AttnA
   const kvr_c8_rows::Plan &p = r->plan;
   const Dims &dm = m->dims;
   const kvr_c8 *c = r->docs[x.doc];
-  const size_t power_b = up256(dm.G * sizeof(float2)),
-               pages_b = x.straight ? 0 : up256((size_t)x.plan.pages * 2 * dm.G * KVR_PAGE * dm.dh * 2),
-               vec = (size_t)dm.G * x.shape.nv_pad;
-  const size_t o_vec = 2 * power_b + pages_b, o_cl = o_vec + vec * dm.dh * 2, o_last = o_cl + vec * 12,
-               o_part = o_last + vec * 4,
-               part_b = x.shape.runs > 1 ? (size_t)x.shape.runs * dm.G * x.shape.keys * 4 : 0,
-               all = stats ? o_part + part_b : o_vec;
-  KVR_TRY(keep_device(m, m->c8_pages, m->c8_pages_bytes, all, "pages of halves"));
-  char *base = (char *)m->c8_pages, *pages = base + 2 * power_b;
+  const size_t vec = (size_t)dm.G * x.shape.nv_pad;
+  const ManyScratch at = many_scratch(dm, x, stats != nullptr);
+  char *base = (char *)m->c8_pages, *pages = base + 2 * at.powers;
   float2 *power = (float2 *)base;
   const void *q = (const char *)a.q + (size_t)x.row0 * a.ldq * dm.es();
   void *out = (char *)a.out + (size_t)x.row0 * dm.H * dm.dh * dm.es();
@@ -351,10 +365,10 @@ kvr_status attend_many(kvr_c8_rows *r, const kvr_c8_rows::Many &x, const C8AttnA
   const int32_t *pos = p.pos_d + x.row0;
   if (stats) stats += (size_t)x.row0 * dm.H;
   // for the weights
-  float *key_power = (float *)(base + power_b), *factor = (float *)(base + o_cl), *minus = factor + vec,
-        *inverse = minus + vec;
-  __half *vectors = (__half *)(base + o_vec);
-  int32_t *last = (int32_t *)(base + o_last);
+  float *key_power = (float *)(base + at.powers), *factor = (float *)(base + at.factors),
+        *minus = factor + vec, *inverse = minus + vec;
+  __half *vectors = (__half *)(base + at.vectors);
+  int32_t *last = (int32_t *)(base + at.last);
   if (x.straight) {
     C8RowsArgs w{};
     w.cache = c->view();
@@ -399,7 +413,7 @@ kvr_status attend_many(kvr_c8_rows *r, const kvr_c8_rows::Many &x, const C8AttnA
   w.stats = stats;
   w.key_power = key_power, w.vectors = vectors;
   w.factor = factor, w.minus = minus, w.inverse = inverse, w.last = last;
-  w.partial = (float *)(base + o_part);
+  w.partial = (float *)(base + at.partial);
   w.weight = c->weight + (size_t)a.layer * dm.G * c->pages * KVR_PAGE;
   w.len = c->len[a.layer];
   w.decay = decay;
@@ -434,6 +448,10 @@ kvr_status attend(kvr_c8_rows *r, int layer, const void *q, int ldq, bool weigh,
     stats = a.stats = (float2 *)m->c8_scores;
     a.scores = (float *)((char *)m->c8_scores + stats_b);
   }
+  // all scratch is there before the first launch: a call that has to be refused leaves nothing behind
+  size_t many = 0;
+  for (const auto &x : p.many) many = std::max(many, many_scratch(dm, x, weigh).all);
+  KVR_TRY(keep_device(m, m->c8_pages, m->c8_pages_bytes, many, "pages of halves"));
   std::vector<int> len;
   for (const auto &x : p.launches) {
     a.settled = r->settled;

@@ -913,6 +913,54 @@ def test_captured_before_any_other_call(models, rows_):
     p.c.close()
 
 
+def test_refused_capture_leaves_nothing():
+    """A captured call whose scratch has not grown: nothing of it is in the graph, of the documents
+    that come before the one that wants it either."""
+    if kv is None:
+        raise _IMPORT_ERROR
+    dh, H, G = SHAPES["dh128"]
+    m = kv.Model(synth.preset("tiny", dtype="bf16", head_dim=dh, n_heads=H, n_kv_heads=G, n_layers=2),
+                 None, seed=0, max_context=256, max_rows=64)
+    m.set_stream(torch.cuda.current_stream().cuda_stream)
+    few = Pair(m, "dh128", "bf16", 100).fill(5, 100)
+    many = Pair(m, "dh128", "bf16", 2000).fill(7, 2000)
+    # few rows' scratch, larger than the call below wants, and none for many rows of a document
+    warm = m.rows8([(few.c, np.sort(np.arange(400) % 100))])
+    qw = queries(8, 400, H, dh, "bf16")
+    warm.attention(0, qw, torch.empty_like(qw), weigh=0.0)
+    r = m.rows8([(few.c, [50]), (many.c, np.arange(1700, 2000))])
+    q = queries(9, 301, H, dh, "bf16")
+    out, mark = torch.full_like(q, 7.0), torch.zeros(8, device="cuda")
+    for d in (few, many):
+        d.c.set_weights(torch.full((2, G, d.c.n), 3.0, device="cuda"))
+    s = torch.cuda.Stream()
+    m.set_stream(s.cuda_stream)
+    try:
+        torch.cuda.synchronize()
+        before = m.launches()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            mark += 1
+            with pytest.raises(kv.KvrError) as e:
+                r.attention(0, q, out, weigh=0.5)
+        assert e.value.code == 6 and m.launches() == before
+        with torch.cuda.stream(s):
+            g.replay()
+        torch.cuda.synchronize()
+        assert (mark == 1).all() and (out == 7).all()
+        for d in (few, many):
+            assert (weights_of(d.c, 0, d.c.n, G) == 3).all()
+        r.attention(0, q, out, weigh=0.5)  # once, as if the refused one had not been
+        m.synchronize()
+    finally:
+        m.set_stream(torch.cuda.current_stream().cuda_stream)
+    check_attention(few, 0, q[:1], [50], out[:1], weights_of(few.c, 0, 100, G), np.full((G, 100), 3.0),
+                    0.5)
+    check_attention(many, 0, q[1:], np.arange(1700, 2000), out[1:], weights_of(many.c, 0, 2000, G),
+                    np.full((G, 2000), 3.0), 0.5)
+    m.close()
+
+
 def test_refusals(models):
     m = models("dh64", "bf16")
     dh, H, G = SHAPES["dh64"]
