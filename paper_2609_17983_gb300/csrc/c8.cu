@@ -26,12 +26,21 @@ constexpr int MAX_ROWS = 1 << 20, MAX_DOCS = 4096;
 // more): half of L2, where the launch that sums them finds them.
 constexpr long long SCORE_BYTES = 64 << 20;
 
-// Memory that a captured launch may hold: what is outgrown is freed with the model.
+// Scratch of at least `need` bytes.  What is outgrown is freed, or with the model once a graph may hold
+// its address.  Growth at least doubles it, so that lengthening documents do not wait at every
+// block, up to 256 MB at once where that leaves no outgrown memory behind.
 kvr_status keep_device(kvr_model *m, void *&buf, size_t &have, size_t need, const char *what) {
   if (need <= have) return KVR_OK;
   KVR_TRY(not_captured(m, "scratch to be allocated (run the call once before)"));
-  if (buf) m->retired.push_back(buf);
-  const size_t size = std::max(need, 2 * have);
+  const size_t more = m->c8_captured ? have : std::min(have, (size_t)256 << 20);
+  if (buf && m->c8_captured) {
+    m->retired.push_back(buf);
+  } else if (buf) {
+    if (cudaStreamSynchronize(m->stream) != cudaSuccess)
+      return fail(KVR_E_CUDA, "%s: %s", what, cudaGetErrorString(cudaGetLastError()));
+    dev_free(buf);
+  }
+  const size_t size = std::max(need, have + more);
   buf = dev_alloc(size);
   have = buf ? size : 0;
   return buf ? KVR_OK : fail(KVR_E_NOMEM, "%s: %zu bytes", what, size);
@@ -496,6 +505,7 @@ kvr_status attention_call(kvr_c8_rows *r, int32_t layer, const void *q, int32_t 
   KVR_TRY(use_device(m));
   KVR_TRY(check_device_ptr(m, q, "q"));
   KVR_TRY(check_device_ptr(m, out, "out"));
+  if (!m->c8_captured) m->c8_captured = capturing(m);  // (0.03 us)
   return attend(r, layer, q, ldq, weigh, decay, out);
 }
 

@@ -289,11 +289,12 @@ struct kvr_model {
   size_t pack_pages_bytes = 0;
   // 8-bit attention: partial sums of split tiles and their arrivals, zero between calls; the
   // scores of vectors that weigh entries, behind what makes weights of them.  Captured launches hold
-  // these addresses, so what is outgrown stays until the model goes.
+  // these addresses, so once there are any (c8_captured) what is outgrown stays until the model goes.
   void *c8_ws = nullptr, *c8_count = nullptr, *c8_scores = nullptr;
   size_t c8_ws_bytes = 0, c8_count_bytes = 0, c8_scores_bytes = 0;
   void *c8_pages = nullptr;  // a layer's pages of a document in halves, and its weights' scratch
   size_t c8_pages_bytes = 0;
+  bool c8_captured = false;
   std::vector<void *> retired;
   int *dev_flag = nullptr;     // device error flag (bounded waits)
   kvr::TraceBuf trace{};       // attached device timeline buffer, if any

@@ -961,6 +961,44 @@ def test_refused_capture_leaves_nothing():
     m.close()
 
 
+def test_outgrown_scratch_is_freed():
+    """Rows of a document, of more of it from call to call: a model that has captured nothing holds as
+    much then as one that made the last call alone."""
+    if kv is None:
+        raise _IMPORT_ERROR
+    dh, H, G, R, ends = 128, 16, 8, 1021, [2600, 5500, 11800, 25000, 53000]
+
+    def grown(ends):
+        m = kv.Model(synth.preset("tiny", dtype="bf16", head_dim=dh, n_heads=H, n_kv_heads=G,
+                                  n_layers=1), None, seed=0, max_context=256, max_rows=64)
+        m.set_stream(torch.cuda.current_stream().cuda_stream)
+        c, at = m.cache8(ends[-1]), 10000
+        for i in range(0, ends[-1], at):
+            n = min(at, ends[-1] - i)
+            k = torch.ones((n, 1, G, dh), dtype=torch.bfloat16, device="cuda")
+            c.write(np.arange(i, i + n), k, k)
+        r = m.rows8([(c, np.arange(R))])
+        q = torch.ones((R, H, dh), dtype=torch.bfloat16, device="cuda")
+        out = torch.empty_like(q)
+        torch.cuda.synchronize()
+        free = torch.cuda.mem_get_info()[0]
+        for e in ends:
+            r.move(np.arange(e - R, e))
+            before = m.launches()
+            r.attention(0, q, out, weigh=0.0)
+            assert (out == 1).all()
+        assert m.launches() - before >= 5  # by way of pages of halves: the most scratch
+        torch.cuda.synchronize()
+        used = free - torch.cuda.mem_get_info()[0]
+        m.close()
+        return used
+
+    grown(ends)  # (all kernels are loaded)
+    last, all_ = grown(ends[-1:]), grown(ends)
+    assert last > 200e6
+    assert all_ - last < 0.1 * last, (last, all_)
+
+
 def test_refusals(models):
     m = models("dh64", "bf16")
     dh, H, G = SHAPES["dh64"]
