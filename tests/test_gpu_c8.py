@@ -948,8 +948,9 @@ def test_refused_capture_leaves_nothing():
             g.replay()
         torch.cuda.synchronize()
         assert (mark == 1).all() and (out == 7).all()
-        for d in (few, many):
-            assert (weights_of(d.c, 0, d.c.n, G) == 3).all()
+        with torch.cuda.stream(s):
+            for d in (few, many):
+                assert (weights_of(d.c, 0, d.c.n, G) == 3).all()
         r.attention(0, q, out, weigh=0.5)  # once, as if the refused one had not been
         m.synchronize()
     finally:

@@ -221,3 +221,53 @@ def test_blocks_far_below_the_largest(models, case, keys, values):
         call.check()
     else:
         call.check(2.0 ** -32 * key_power, 2.0 ** -32 * value_power)
+
+
+@pytest.mark.parametrize("case", list(CASES))
+@pytest.mark.parametrize("decay", [0.5, 1.0])
+def test_entries_far_behind_the_last_row(models, case, decay):
+    """Whole tiles of keys, and several CTAs' runs of them, that no row sees: their weights decay."""
+    way, split, dh, H, G, n, R, spread = CASES[case]
+    m, behind = models(dh, H, G), 4099
+    k, v = normal(11, n + behind, G, dh), normal(12, n + behind, G, dh)
+    old = torch.rand((G, n + behind), generator=torch.Generator().manual_seed(13)).cuda()
+    call = Call(m, case, k, v, normal(14, R + 1, H, dh), old, decay)
+    call.check()
+    assert torch.equal(call.weight[:, n:], (old[:, n:] * decay).double())
+
+
+@pytest.mark.parametrize("case", list(CASES))
+def test_captured_and_replayed(models, case):
+    """The first call of rows that have just been moved, captured: a replay is the call."""
+    way, split, dh, H, G, n, R, spread = CASES[case]
+    m = models(dh, H, G)
+    c = filled(m, normal(15, n, G, dh), normal(16, n, G, dh))
+    seen, q = places(n, R, spread), normal(17, R, H, dh)
+    want, out = torch.empty_like(q), torch.full_like(q, 7.0)
+    s = torch.cuda.Stream()
+    try:
+        torch.cuda.synchronize()
+        m.set_stream(s.cuda_stream)
+        first = m.rows8([(c, seen)])
+        first.attention(0, q, want, weigh=0.0)  # (the scratch grows)
+        first.attention(0, q, want, weigh=1.0)
+        with torch.cuda.stream(s):
+            twice = weights(c, n, G)
+        r = m.rows8([(c, np.zeros(R, int))])
+        m.synchronize()
+        r.move(seen)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            r.attention(0, q, out, weigh=0.0)
+            r.attention(0, q, out, weigh=1.0)
+        with torch.cuda.stream(s):
+            g.replay()
+            g.replay()
+        m.synchronize()
+        torch.cuda.synchronize()
+    finally:
+        m.set_stream(torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(out, want) and torch.equal(weights(c, n, G), twice)
+    r.close()
+    first.close()
+    c.close()
