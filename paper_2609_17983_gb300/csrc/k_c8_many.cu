@@ -237,13 +237,13 @@ __device__ __forceinline__ void tmem_ld8_nowait(uint32_t taddr, uint32_t *r) {
 // What it saves beside the way by pages of halves are those pages: written once and read by every
 // tile, three times the codes' bytes and a launch.  What bounds it is shared memory, 224 KB a step
 // (codes in and out, halves in, the products' operands), beside the chain from scores to weights: a
-// step takes 1.05 us (512 rows of 32 heads over 5000 entries, 128 CTAs of 40 steps, 46.3; 64 over
-// 16384, 9 parts of 15 steps and their sum, 26.0; with a step's weights under the old reference taken
+// step takes 1.05 us (512 rows of 32 heads over 5000 entries, 128 CTAs of 40 steps, 46.6; 64 over
+// 16384, 9 parts of 15 steps and their sum, 26.6; with a step's weights under the old reference taken
 // beside its maximum, and again where that is not enough, 48.8 and 27.8).  Parts that a cluster adds
 // in its shared memory save the other launch (128 rows over 5000, clusters of 4: 20.7 for 23.6), but
 // 16 clusters of 8 do not run at once, and smaller ones have longer parts (64 rows over 16384: 32.3):
 // left out.  For weights of the entries it leaves its queries as halves, with what makes weights of
-// their products (by a kernel of their own 45.2 us for 64 rows over 16384, 44.0 so).
+// their products (by a kernel of their own 45.2 us for 64 rows over 16384, 44.3 so).
 template <int DH>
 __global__ void __launch_bounds__(NTR, 1) k_c8_rows(const __grid_constant__ C8RowsArgs p) {
   constexpr int HALVES = DH / 64;
